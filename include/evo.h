@@ -530,6 +530,151 @@ int evo_debug_encoder_plan(const evo_encoder_desc* desc, int32_t batch, int32_t 
 /* Release the encoder (NULL is a no-op); synchronises its device first. */
 void evo_destroy_encoder(evo_encoder* e);
 
+/* ---- Long memories ----------------------------------------------------
+ * A policy may be conditioned on more memory tokens than the compiled loop
+ * keeps beside its samples (image patches, language, a long history).  Their
+ * keys and values do not change while an action chunk is denoised (Sec. 3.4:
+ * caches live for one action query), so they are written once into a paged
+ * cache and attended to at every evaluated step (Eq. 1) by the chunk's tokens.
+ *
+ * The cache's memory belongs to the caller:
+ *   k  [n_pages][n_kv_heads][page_size][head_dim]
+ *   v  [n_pages][n_kv_heads][head_dim][page_size]
+ *   k_scale, v_scale  float [n_pages][n_kv_heads][page_size], 8-bit formats
+ *     only (NULL otherwise)
+ * Values lie transposed because a cache is written once and read at every
+ * step: the attention's second product then takes its operand straight from
+ * memory.  Position p of a sequence lies in slot p % page_size of page
+ * page_table[p / page_size] of that sequence; pages may be shared and lie in
+ * any order.  All four arrays 16-byte aligned.
+ *
+ * Formats: fp32 and bf16 hold values; int8 and fp8 (e4m3, largest value 448)
+ * hold codes of x / s rounded to nearest, ties to even, with one scale
+ * s = max|x| / 127 or / 448 for each token and head (s = 0 for a row of
+ * zeros).  A row that holds a NaN or an infinity gets s = NaN: it reads back
+ * as NaN and makes the outputs of the queries that see it NaN. */
+enum { EVO_CACHE_FP32 = 0, EVO_CACHE_BF16 = 1, EVO_CACHE_INT8 = 2, EVO_CACHE_FP8 = 3 };
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t format;      /* EVO_CACHE_* */
+  int32_t n_pages;
+  int32_t page_size;   /* 64, 128, 256, 512 or 1024 */
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 32, 64 or 128 */
+} evo_kv_cache;
+
+/* The rows (tokens) of a call: sequence s has rows cu_rows[s] ..
+ * cu_rows[s + 1] - 1 of the call's n_rows, at most max_rows of them (device
+ * int32 [n_seqs + 1], ascending from 0 to n_rows; NULL: every sequence has
+ * max_rows rows and n_rows == n_seqs * max_rows).  page_table: device int32
+ * [n_seqs][max_pages].  What the device arrays hold is not checked on the
+ * host; the kernels keep every access inside the caller's arrays whatever
+ * they hold (pages outside the cache are taken as its last page, positions
+ * beyond max_pages * page_size are not written and read as zeros). */
+typedef struct {
+  int32_t n_seqs, n_rows, max_rows, max_pages;
+  const int32_t* cu_rows;
+  const int32_t* page_table;
+} evo_kv_rows;
+
+/* A tensor [rows][heads][head_dim]: strides in elements, the last dimension
+ * contiguous (views of a packed projection output are fine).  Rows aligned to
+ * 16 bytes take the wide loads. */
+typedef struct {
+  void* data;
+  int64_t row_stride, head_stride;
+} evo_heads;
+
+/* Norm of queries and keys for each head, and the rotation by position:
+ *   y = x / sqrt(mean(x^2) + eps) * gain    (eps < 0: y = x, gains unused)
+ * then pairs (a, b) of the first rotary_dim values become
+ * (a cos - b sin, b cos + a sin) with the table's (cos, sin) of the row's
+ * position and the pair; the other values pass. */
+enum { EVO_PAIRS_HALVES = 0,    /* pair i: values i and i + rotary_dim / 2 */
+       EVO_PAIRS_ADJACENT = 1 };/* pair i: values 2i and 2i + 1 */
+typedef struct {
+  int32_t rotary_dim;    /* 0 (no rotation) or a multiple of 16 up to head_dim */
+  int32_t pairs;         /* EVO_PAIRS_* */
+  int32_t n_positions;   /* rows of the table; a position outside it makes its row NaN */
+  float eps;
+  const float* q_gain;   /* device [head_dim], or NULL for ones */
+  const float* k_gain;
+  const float* table;    /* device [n_positions][rotary_dim / 2][2] = (cos, sin), 16-byte aligned */
+} evo_norm_rope;
+
+/* Normalise and rotate queries and keys.  dtype (of q, k and the outputs):
+ * EVO_FP32 or EVO_BF16; all arithmetic fp32, rounded once.  positions: device
+ * int32 [n_rows].  Outputs may be the inputs.  n_heads or n_kv_heads may be 0
+ * (that tensor is then ignored).  Asynchronous on hip_stream; the device
+ * memory belongs to the current device. */
+int evo_qk_norm_rope(const evo_norm_rope* nr, int32_t dtype, int32_t head_dim, int32_t n_rows, int32_t n_heads,
+                     int32_t n_kv_heads, const evo_heads* q, const evo_heads* k, const int32_t* positions,
+                     const evo_heads* q_out, const evo_heads* k_out, void* hip_stream);
+
+/* Write keys and values (dtype EVO_FP32 or EVO_BF16) into the cache: row i of
+ * sequence s at position starts[s] + i (device int32 [n_seqs]).  Rows of one
+ * call must not share a slot.  A fp32 cache takes fp32 rows, a bf16 cache bf16
+ * rows, the 8-bit formats both. */
+int evo_cache_write(const evo_kv_cache* cache, const evo_kv_rows* rows, int32_t dtype, const int32_t* starts,
+                    const evo_heads* k, const evo_heads* v, void* hip_stream);
+
+/* Read positions back as values of dtype (pairs of formats as for
+ * evo_cache_write): row i of sequence s is position starts[s] + i.  k_out and
+ * v_out must not overlap. */
+int evo_cache_read(const evo_kv_cache* cache, const evo_kv_rows* rows, int32_t dtype, const int32_t* starts,
+                   const evo_heads* k_out, const evo_heads* v_out, void* hip_stream);
+
+/* evo_qk_norm_rope and evo_cache_write in one launch, as a layer does with the
+ * output of its projection: q (n_heads) normalised and rotated into q_out, k
+ * normalised, rotated and written (rounded once, to the cache's format), v
+ * written.  Rotation by the positions that are written. */
+int evo_qkv_write(const evo_kv_cache* cache, const evo_kv_rows* rows, const evo_norm_rope* nr, int32_t dtype,
+                  int32_t n_heads, const int32_t* starts, const evo_heads* q, const evo_heads* k, const evo_heads* v,
+                  const evo_heads* q_out, void* hip_stream);
+
+/* Attention of a chunk of new tokens over the cache.  Row i of sequence s is
+ * at position p_i = starts[s] + i (NULL: starts[s] = lengths[s] - rows of s,
+ * so the chunk is the cache's end); its keys are positions j < lengths[s].
+ *   z_ij = scale q_i . k_j; cap > 0: z = cap tanh(z / cap);
+ *   slopes: z = z - slopes[head] |p_i - j|
+ *   visible: j < prefix[s], or
+ *            (not causal or j <= p_i) and (window == 0 or |p_i - j| < window)
+ *   out_i = sum_j softmax_j(z_ij) v_j over the visible j,
+ *   lse_i = log sum_j exp(z_ij); where nothing is visible out 0, lse -inf.
+ * What a row does not see does not reach its output, whatever it holds.
+ * Query head h reads key/value head h / (n_heads / n_kv_heads).  Statistics
+ * and sums are fp32; with EVO_BF16 the products take bf16 operands (8-bit
+ * codes are exact in bf16; the softmax's terms are rounded to bf16 for the
+ * second product), with EVO_FP32 fp32 operands. */
+typedef struct {
+  int32_t dtype;           /* of q and out; pairs of formats as for evo_cache_write */
+  int32_t n_heads;         /* a multiple of the cache's n_kv_heads */
+  int32_t causal;          /* 0 or 1 */
+  int32_t window;          /* 0: none */
+  int32_t max_length;      /* no sequence is longer; 0: max_pages * page_size */
+  float scale, cap;        /* cap 0: none */
+  const int32_t* lengths;  /* device [n_seqs] */
+  const int32_t* starts;   /* device [n_seqs] or NULL */
+  const int32_t* prefix;   /* device [n_seqs] or NULL */
+  const float* slopes;     /* device [n_heads] or NULL */
+} evo_attention;
+
+/* Bytes of device workspace that evo_chunk_attention needs for these
+ * arguments on the current device (0: none), or a negative EVO_E_* code.  The
+ * device pointers of the arguments are not read. */
+int64_t evo_chunk_attention_workspace(const evo_kv_cache* cache, const evo_kv_rows* rows, const evo_attention* att);
+
+/* q, out: [n_rows][n_heads][head_dim]; lse: device float [n_rows][n_heads] or
+ * NULL.  workspace: device memory, 16-byte aligned, of at least the bytes
+ * above, in use until the enqueued work completes (NULL if 0).  Results do not
+ * depend on what the workspace held, and are the same at every call. */
+int evo_chunk_attention(const evo_kv_cache* cache, const evo_kv_rows* rows, const evo_attention* att,
+                        const evo_heads* q, const evo_heads* out, float* lse, void* workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
 /* Thread-local message of the last failed call on this thread. */
 const char* evo_last_error(void);
 

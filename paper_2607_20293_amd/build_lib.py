@@ -15,7 +15,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libevo.so")
 DEMO = os.path.join(HERE, "evo_demo")
 SOURCES = ["evo_host.cpp", "evo_ga.cpp", "evo_kernels.hip", "evo_redundancy.hip", "evo_search.hip", "evo_encoder.hip",
-           "evo_api.hip"]
+           "evo_api.hip", "evo_memory.hip", "evo_memory_rows.hip", "evo_memory_attention.hip"]
 ARCH = os.environ.get("EVO_OFFLOAD_ARCH", "gfx950")
 
 

@@ -1,0 +1,111 @@
+// Interface between the long-memory entry points (evo_memory.hip) and their
+// kernels: rows of queries, keys and values (evo_memory_rows.hip) and
+// attention over the paged cache (evo_memory_attention.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace evo {
+
+// The paged cache (layout: evo.h).  All pages of one head are page_size slots;
+// page_size is 1 << page_shift.
+struct CacheView {
+  void* k;
+  void* v;
+  float* ks;
+  float* vs;
+  int n_pages, page_shift, n_kv_heads;
+};
+
+// Which rows belong to which sequence; cu == NULL: max_rows each.
+struct RowsView {
+  const int32_t* cu;
+  const int32_t* pages;   // [n_seqs][max_pages]
+  int n_seqs, n_rows, max_rows, max_pages;
+};
+
+struct HeadsView {
+  char* p;
+  int64_t row, head;      // strides in elements
+};
+
+// One launch over rows: norm and rotation of q and k, k and v into the cache.
+struct RowsArgs {
+  HeadsView q, k, v, qo, ko;  // ko: keys that do not go to the cache
+  int n_heads, n_kv_heads;
+  int heads_per_group;        // heads that a group of lanes works through
+  int norm, half, adjacent, n_positions;
+  float eps;
+  const float* q_gain;
+  const float* k_gain;
+  const float* table;
+  const int32_t* positions;   // NULL: the positions that are written
+  const int32_t* starts;
+  CacheView cache;
+  RowsView rows;
+  int wide;                   // every row 16-byte aligned
+  int qk_blocks;              // workgroups of the q and k part
+};
+
+// format: EVO_CACHE_*, or -1 with no cache (keys to ko).  dtype: EVO_FP32 / EVO_BF16.
+hipError_t launch_rows(int dtype, int format, int head_dim, RowsArgs a, hipStream_t stream);
+hipError_t launch_cache_read(int dtype, int format, int head_dim, RowsArgs a, hipStream_t stream);
+
+struct AttArgs {
+  HeadsView q, out;
+  float* lse;                 // [n_rows][n_heads] or NULL
+  CacheView cache;
+  RowsView rows;
+  const int32_t* lengths;
+  const int32_t* starts;      // NULL: lengths - rows
+  const int32_t* prefix;      // or NULL
+  const float* slopes;        // or NULL
+  int n_heads, group;         // group: query heads per key/value head
+  int causal, window;
+  float scale, cap;
+  int wide;                   // rows of q and out 16-byte aligned
+  // plan
+  int tiles_per_seq;          // 0: a sequence's tiles start at row / tile + sequence
+  int n_tiles;                // row tiles over all sequences
+  int n_split;                // parts of the keys
+  float* part;                // [n_tiles][n_kv_heads][n_split][tile rows][head_dim] unnormalised outputs
+  float* part_ml;             // [n_tiles][n_kv_heads][n_split][tile rows][2]: maximum (log2), sum
+};
+
+struct AttPlan {
+  int tile_rows, tiles_per_seq, n_tiles, n_split;
+  int64_t part_floats, ml_floats;
+};
+
+AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_kv_heads, const RowsView& r,
+                       int max_length, int window, bool causal, int n_cu);
+hipError_t launch_attention(int dtype, int format, int head_dim, const AttPlan& plan, const AttArgs& a,
+                            hipStream_t stream);
+
+// The sequence of row n and the row's place in it.
+__device__ __forceinline__ void find_row(const RowsView& r, int n, int* seq, int* i) {
+  if (!r.cu) {
+    const int s = n / r.max_rows;
+    *seq = s;
+    *i = n - s * r.max_rows;
+    return;
+  }
+  int lo = 0, hi = r.n_seqs;  // the last sequence that starts at or before n
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (r.cu[mid] <= n) lo = mid;
+    else hi = mid;
+  }
+  *seq = lo;
+  *i = n - r.cu[lo];
+}
+
+// The page of a position that lies below max_pages << page_shift.
+__device__ __forceinline__ int page_of(const RowsView& r, const CacheView& c, int seq, int page_index) {
+  const unsigned pg = (unsigned)r.pages[(int64_t)seq * r.max_pages + page_index];
+  return (int)min(pg, (unsigned)(c.n_pages - 1));
+}
+
+}  // namespace evo

@@ -1,0 +1,744 @@
+// Attention of a chunk of new tokens over the paged cache of keys and values,
+// with the softmax's running maximum and sum, in one pass over the cache.
+//
+// A workgroup takes a tile of 16 R rows (tokens x the query heads that share a
+// key/value head) and a part of the keys; its four waves take blocks of 64
+// keys in turn and join at the end.  Products are formed transposed, S^T = K
+// Q^T and O^T = V^T P^T:
+//  * a lane of the first product's result holds one row's scores, so scaling,
+//    masks and the running maximum and sum are lane-local, apart from two
+//    exchanges over the four lane groups that share a row;
+//  * the keys of a block are dealt to the matrix rows in the order (key_of)
+//    that leaves each lane with the run of keys that the second product wants
+//    from it, so scores become its operand without leaving the lane;
+//  * with transposed value pages every operand of K and V is a 16-byte load
+//    from memory to registers: nothing goes through LDS in the loop.
+// The next block's keys are requested when the first product has taken this
+// block's, the next values when the second has.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "evo.h"
+#include "evo_memory.hpp"
+
+namespace evo {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kKeys = 64;     // keys of a block
+constexpr int kWaves = 4;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_inff();
+
+constexpr bool is_coded(int f) { return f == EVO_CACHE_INT8 || f == EVO_CACHE_FP8; }
+constexpr int size_of(int f) { return f == EVO_CACHE_FP32 ? 4 : f == EVO_CACHE_BF16 ? 2 : 1; }
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// maximum / sum over the four lanes lane % 16 of a wave
+__device__ __forceinline__ float over_groups(float x, bool maximum) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const float a0 = __builtin_bit_cast(float, (uint32_t)a[0]), a1 = __builtin_bit_cast(float, (uint32_t)a[1]);
+  const float y = maximum ? fmaxf(a0, a1) : a0 + a1;
+  const uint32_t w = __builtin_bit_cast(uint32_t, y);
+  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  const float b0 = __builtin_bit_cast(float, (uint32_t)b[0]), b1 = __builtin_bit_cast(float, (uint32_t)b[1]);
+  return maximum ? fmaxf(b0, b1) : b0 + b1;
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// four codes to bf16 (exact: codes have at most 8 significant bits)
+template <int F> __device__ __forceinline__ u32x2 codes_bf16(uint32_t v) {
+  if (F == EVO_CACHE_FP8)
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, true))};
+  return u32x2{pack2((float)(int8_t)v, (float)(int8_t)(v >> 8)), pack2((float)(int8_t)(v >> 16), (float)(int8_t)(v >> 24))};
+}
+template <int F> __device__ __forceinline__ float code_f32(uint32_t v, int e) {
+  if (F == EVO_CACHE_FP8) {
+    const auto a = e < 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(v, false) : __builtin_amdgcn_cvt_pk_f32_fp8(v, true);
+    return a[e & 1];
+  }
+  return (float)(int8_t)(v >> (8 * e));
+}
+
+// How a lane's share of a block lies, by format.  E: consecutive values of a
+// key row per load; KG: consecutive keys per load of a value row.
+template <int F, int DH> struct Lay {
+  static constexpr int SZ = size_of(F);
+  static constexpr int E = 16 / SZ < DH / 4 ? 16 / SZ : DH / 4;
+  static constexpr int KL = DH / (4 * E);        // loads of a key row
+  static constexpr int KW = DH * SZ / 16;        // dwords of a key row
+  static constexpr int KG = 16 / SZ;
+  static constexpr int VL = 16 / KG;             // loads of a value row (16 keys)
+  static constexpr int VW = 4 * SZ;              // dwords of a value row
+  static constexpr int CT = DH / 16;             // tiles of channels
+  // the key (in its block) of row 4 g + i of score tile t
+  __device__ static constexpr int key_of(int t, int g, int i) {
+    constexpr int U = KG / 4;
+    return (t / U) * (4 * KG) + g * KG + (t % U) * 4 + i;
+  }
+};
+
+struct Where {
+  int row0, rows, base, p_first, p_last, ctx, start, prefix;
+};
+
+// The row tile of a workgroup; false if it has no rows.
+__device__ __forceinline__ bool find_tile(const AttArgs& a, int tile, int tile_rows, int* seq_out, Where* w) {
+  int seq, j;
+  if (a.tiles_per_seq) {
+    seq = tile / a.tiles_per_seq;
+    j = tile - seq * a.tiles_per_seq;
+  } else {
+    int lo = 0, hi = a.rows.n_seqs;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.rows.cu[mid] * a.group / tile_rows + mid <= tile) lo = mid;
+      else hi = mid;
+    }
+    seq = lo;
+    j = tile - (a.rows.cu[lo] * a.group / tile_rows + lo);
+  }
+  int r0, n;
+  if (a.rows.cu) {
+    r0 = min(max(a.rows.cu[seq], 0), a.rows.n_rows);
+    n = min(min(max(a.rows.cu[seq + 1], r0), a.rows.n_rows) - r0, a.rows.max_rows);
+  } else {
+    r0 = seq * a.rows.max_rows;
+    n = a.rows.max_rows;
+  }
+  if (j < 0 || j * tile_rows >= n * a.group) return false;
+  w->row0 = r0;
+  w->rows = n * a.group;
+  w->base = j * tile_rows;
+  w->ctx = min(max(a.lengths[seq], 0), a.rows.max_pages << a.cache.page_shift);
+  w->start = a.starts ? min(max(a.starts[seq], -(1 << 29)), 1 << 29) : w->ctx - n;
+  w->prefix = a.prefix ? min(max(a.prefix[seq], 0), w->ctx) : 0;
+  w->p_first = w->start + w->base / a.group;
+  w->p_last = w->start + (min(w->base + tile_rows, w->rows) - 1) / a.group;
+  *seq_out = seq;
+  return true;
+}
+
+// The blocks that some row of the tile sees: the prefix's, then lo .. hi - 1.
+struct Blocks {
+  int n_prefix, lo, count;
+  __device__ int at(int v) const { return v < n_prefix ? v : v - n_prefix + lo; }
+};
+__device__ __forceinline__ Blocks blocks_of(const AttArgs& a, const Where& w) {
+  int hi = w.ctx, lo = 0;
+  if (a.causal) hi = min(hi, w.p_last + 1);
+  if (a.window) {
+    hi = min(hi, w.p_last + a.window);
+    lo = max(0, w.p_first - a.window + 1);
+  }
+  Blocks b;
+  b.n_prefix = (w.prefix + kKeys - 1) / kKeys;
+  b.lo = max(lo / kKeys, b.n_prefix);
+  b.count = b.n_prefix + (hi > lo ? max(0, (hi + kKeys - 1) / kKeys - b.lo) : 0);
+  return b;
+}
+
+__device__ __forceinline__ bool sees(const AttArgs& a, const Where& w, int p, int j) {
+  const bool near = (!a.causal || j <= p) && (!a.window || abs(p - j) < a.window);
+  return j < w.ctx && (j < w.prefix || near);
+}
+// whether every row of the tile sees every key of block kb .. kb + 63
+__device__ __forceinline__ bool sees_all(const AttArgs& a, const Where& w, int kb) {
+  const int ke = kb + kKeys - 1;
+  const bool near = (!a.causal || ke <= w.p_first) &&
+                    (!a.window || (w.p_last - kb < a.window && ke - w.p_first < a.window));
+  return ke < w.ctx && (ke < w.prefix || near);
+}
+
+template <typename T> __device__ __forceinline__ float squash(float x);
+// Behind bf16 products the absolute error of 2^-23 near 0 is far below theirs.
+template <> __device__ __forceinline__ float squash<__bf16>(float x) {
+  return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_(x * (2.f * kLog2e)));
+}
+template <> __device__ __forceinline__ float squash<float>(float x) { return tanhf(x); }
+
+template <typename T, int DH> struct Query;
+template <int DH> struct Query<__bf16, DH> { bf16x8 f[DH / 32]; };
+template <int DH> struct Query<float, DH> { float f[DH / 4]; };
+
+// This lane's share of a query row, in the order of the key loads.
+template <int F, int DH>
+__device__ __forceinline__ void load_query(Query<__bf16, DH>& q, const __bf16* p, int g, int wide) {
+  typedef Lay<F, DH> L;
+#pragma unroll
+  for (int k = 0; k < DH / 32; ++k) {
+    const __bf16* s = p + (k / (L::E / 8)) * (4 * L::E) + g * L::E + (k % (L::E / 8)) * 8;
+    if (wide) q.f[k] = *reinterpret_cast<const bf16x8*>(s);
+    else
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q.f[k][e] = s[e];
+  }
+}
+template <int F, int DH>
+__device__ __forceinline__ void load_query(Query<float, DH>& q, const float* p, int g, int wide) {
+  typedef Lay<F, DH> L;
+#pragma unroll
+  for (int l = 0; l < L::KL; ++l)
+#pragma unroll
+    for (int e = 0; e < L::E; ++e) q.f[l * L::E + e] = p[l * 4 * L::E + g * L::E + e];
+}
+
+// S^T += K Q^T for one tile of 16 keys
+template <int F, int DH>
+__device__ __forceinline__ f32x4 score_tile(const uint32_t* k, const Query<__bf16, DH>& q) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < DH / 32; ++j) {
+    u32x4 w;
+    if constexpr (is_coded(F)) {
+      const u32x2 a = codes_bf16<F>(k[2 * j]), b = codes_bf16<F>(k[2 * j + 1]);
+      w = u32x4{a[0], a[1], b[0], b[1]};
+    } else {
+      w = u32x4{k[4 * j], k[4 * j + 1], k[4 * j + 2], k[4 * j + 3]};
+    }
+    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q.f[j], s, 0, 0, 0);
+  }
+  return s;
+}
+template <int F, int DH>
+__device__ __forceinline__ f32x4 score_tile(const uint32_t* k, const Query<float, DH>& q) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < DH / 4; ++j) {
+    float x;
+    if constexpr (is_coded(F)) x = code_f32<F>(k[j / 4], j & 3);
+    else x = __builtin_bit_cast(float, k[j]);
+    s = __builtin_amdgcn_mfma_f32_16x16x4f32(x, q.f[j], s, 0, 0, 0);
+  }
+  return s;
+}
+
+// The second product's operand made of a row's 16 terms of a block.
+template <typename T> struct Terms;
+template <> struct Terms<__bf16> {
+  bf16x8 f[2];
+  __device__ __forceinline__ void set(const float (&p)[4][4]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const u32x4 w = {pack2(p[2 * s][0], p[2 * s][1]), pack2(p[2 * s][2], p[2 * s][3]),
+                       pack2(p[2 * s + 1][0], p[2 * s + 1][1]), pack2(p[2 * s + 1][2], p[2 * s + 1][3])};
+      f[s] = __builtin_bit_cast(bf16x8, w);
+    }
+  }
+};
+template <> struct Terms<float> {
+  float f[4][4];
+  __device__ __forceinline__ void set(const float (&p)[4][4]) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[t][i] = p[t][i];
+  }
+};
+
+// O^T += V^T P^T for one tile of 16 channels
+template <int F>
+__device__ __forceinline__ f32x4 value_tile(const uint32_t* v, const Terms<__bf16>& p, f32x4 o) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    u32x4 w;
+    if constexpr (is_coded(F)) {
+      const u32x2 a = codes_bf16<F>(v[2 * s]), b = codes_bf16<F>(v[2 * s + 1]);
+      w = u32x4{a[0], a[1], b[0], b[1]};
+    } else {
+      w = u32x4{v[4 * s], v[4 * s + 1], v[4 * s + 2], v[4 * s + 3]};
+    }
+    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), p.f[s], o, 0, 0, 0);
+  }
+  return o;
+}
+template <int F>
+__device__ __forceinline__ f32x4 value_tile(const uint32_t* v, const Terms<float>& p, f32x4 o) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x;
+      if constexpr (is_coded(F)) x = code_f32<F>(v[t], i);
+      else x = __builtin_bit_cast(float, v[4 * t + i]);
+      o = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p.f[t][i], o, 0, 0, 0);
+    }
+  return o;
+}
+
+// What a masked block's values may hold where a row does not see them: keys
+// past the cache's length become 0 (a page's unused end may hold anything).
+// Returns, for formats that can hold them, whether a NaN or infinity is left.
+template <int F, int DH, int CT, int VW>
+__device__ __forceinline__ bool clear_tail(uint32_t (&v)[CT][VW], int g, int left) {
+  typedef Lay<F, DH> L;
+  static_assert(CT == L::CT && VW == L::VW, "a lane's values of a block");
+  bool bad = false;
+#pragma unroll
+  for (int l = 0; l < L::VL; ++l)
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const int key = l * (4 * L::KG) + g * L::KG + d * (4 / L::SZ);  // first key of the dword
+      uint32_t keep = 0;
+#pragma unroll
+      for (int e = 0; e < 4 / L::SZ; ++e)
+        if (key + e < left) keep |= (L::SZ == 4 ? 0xffffffffu : ((1u << (8 * L::SZ)) - 1) << (8 * L::SZ * e));
+#pragma unroll
+      for (int c = 0; c < L::CT; ++c) {
+        uint32_t& x = v[c][l * 4 + d];
+        x &= keep;
+        if constexpr (F == EVO_CACHE_FP32) bad |= (x & 0x7f800000u) == 0x7f800000u;
+        if constexpr (F == EVO_CACHE_BF16) bad |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+        if constexpr (F == EVO_CACHE_FP8) bad |= (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+      }
+    }
+  return bad;
+}
+
+// v with its NaNs and infinities replaced: by 0 (which = 0), or 1 where it is
+// +infinity or NaN (which = 1), -infinity or NaN (which = 2) and 0 elsewhere.
+// (A cache that was written holds no NaN codes; unwritten memory may.)
+template <int F> __device__ __forceinline__ uint32_t only(uint32_t x, int which) {
+  if constexpr (F == EVO_CACHE_FP8) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t y = (x >> (8 * e)) & 0xffu;
+      const bool nan = (y & 0x7fu) == 0x7fu;
+      r |= (which == 0 ? (nan ? 0 : y) : (nan ? 0x38u : 0)) << (8 * e);  // 0x38: 1
+    }
+    return r;
+  }
+  if constexpr (F == EVO_CACHE_FP32) {
+    const bool bad = (x & 0x7f800000u) == 0x7f800000u, nan = bad && (x & 0x7fffffu);
+    if (which == 0) return bad ? 0 : x;
+    return bad && (nan || (x >> 31) == (uint32_t)(which - 1)) ? 0x3f800000u : 0;
+  } else {
+    uint32_t r = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t y = (x >> (16 * e)) & 0xffffu;
+      const bool bad = (y & 0x7f80u) == 0x7f80u, nan = bad && (y & 0x7fu);
+      const uint32_t z = which == 0 ? (bad ? 0 : y) : (bad && (nan || (y >> 15) == (uint32_t)(which - 1)) ? 0x3f80u : 0);
+      r |= z << (16 * e);
+    }
+    return r;
+  }
+}
+
+template <typename T> __device__ __forceinline__ void store4(T* p, int wide, f32x4 x) {
+  if (sizeof(T) == 4) {
+    if (wide) *reinterpret_cast<f32x4*>(p) = x;
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = (T)x[e];
+  } else {
+    if (wide) *reinterpret_cast<u32x2*>(p) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = (T)x[e];
+  }
+}
+
+// Workgroup (row tile, key/value head, part of the keys).
+template <typename T, int F, int DH, int R>
+__global__ void __launch_bounds__(kWaves * 64) stream_kernel(AttArgs a) {
+  typedef Lay<F, DH> L;
+  constexpr int TR = 16 * R;
+  __shared__ __attribute__((aligned(16))) float join_o[2][TR * DH];
+  __shared__ float join_ml[kWaves][TR][2];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x % a.n_split, th = blockIdx.x / a.n_split;
+  const int h = th % a.cache.n_kv_heads, tile = th / a.cache.n_kv_heads;
+  int seq;
+  Where wh;
+  if (!find_tile(a, tile, TR, &seq, &wh)) return;
+  const Blocks bl = blocks_of(a, wh);
+  const int per = max((bl.count + a.n_split - 1) / a.n_split, kWaves);
+  const int v0 = split * per, v1 = min(v0 + per, bl.count);
+  const int ps = a.cache.page_shift;
+
+  Query<T, DH> q[R];
+  int pos[R];
+  float slope[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = min(wh.base + r * 16 + lr, wh.rows - 1), tok = row / a.group, head = h * a.group + row - tok * a.group;
+    pos[r] = wh.start + tok;
+    slope[r] = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    load_query<F, DH>(q[r], reinterpret_cast<const T*>(a.q.p) + (wh.row0 + tok) * a.q.row + head * a.q.head, g, a.wide);
+  }
+  f32x4 o[R][L::CT];
+  float m[R], l[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -kInf;
+    l[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < L::CT; ++c) o[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float to_log2 = a.scale * kLog2e, to_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, cap_log2 = a.cap * kLog2e;
+
+  // byte offsets of this lane in a block's keys and values
+  const uint32_t koff = (uint32_t)((L::key_of(0, lr >> 2, lr & 3) * DH + g * L::E) * L::SZ);
+  const uint32_t voff = (uint32_t)(((lr << ps) + g * L::KG) * L::SZ);
+  uint32_t kr[4][L::KW], vr[L::CT][L::VW];
+  const auto block_base = [&](int kb, int* slot) -> int64_t {
+    *slot = kb & ((1 << ps) - 1);
+    return (int64_t)page_of(a.rows, a.cache, seq, kb >> ps) * a.cache.n_kv_heads + h;
+  };
+  const auto load_keys = [&](int kb) {
+    int slot;
+    const int64_t b = block_base(kb, &slot);
+    const char* p = reinterpret_cast<const char*>(a.cache.k) + ((b << ps) + slot) * (DH * L::SZ);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < L::KL; ++i) {
+        const char* s = p + koff + ((L::key_of(t, 0, 0) * DH + i * 4 * L::E) * L::SZ);
+        if constexpr (L::E * L::SZ == 16) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(s);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) kr[t][i * 4 + e] = x[e];
+        } else {
+          const u32x2 x = *reinterpret_cast<const u32x2*>(s);
+          kr[t][i * 2] = x[0];
+          kr[t][i * 2 + 1] = x[1];
+        }
+      }
+  };
+  const auto load_values = [&](int kb) {
+    int slot;
+    const int64_t b = block_base(kb, &slot);
+    const char* p = reinterpret_cast<const char*>(a.cache.v) + (((b * DH) << ps) + slot) * L::SZ;
+#pragma unroll
+    for (int c = 0; c < L::CT; ++c)
+#pragma unroll
+      for (int i = 0; i < L::VL; ++i) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(p + voff + (((c * 16) << ps) + i * 4 * L::KG) * L::SZ);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vr[c][i * 4 + e] = x[e];
+      }
+  };
+
+  int v = v0 + w;
+  if (v < v1) {
+    load_keys(bl.at(v) * kKeys);
+    load_values(bl.at(v) * kKeys);
+  }
+  for (; v < v1; v += kWaves) {
+    const int kb = bl.at(v) * kKeys, next = v + kWaves < v1 ? bl.at(v + kWaves) * kKeys : -1;
+    const bool masked = !sees_all(a, wh, kb);
+    float ks[4][4], vs[4][4];
+    if constexpr (is_coded(F)) {
+      int slot;
+      const int64_t at = (block_base(kb, &slot) << ps) + slot;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(a.cache.ks + at + L::key_of(t, g, 0));
+        const f32x4 y = *reinterpret_cast<const f32x4*>(a.cache.vs + at + L::key_of(t, g, 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { ks[t][i] = x[i]; vs[t][i] = y[i]; }
+      }
+    }
+    f32x4 s[R][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < R; ++r) s[r][t] = score_tile<F, DH>(kr[t], q[r]);
+    __builtin_amdgcn_sched_barrier(0);
+    if (next >= 0) load_keys(next);
+    __builtin_amdgcn_sched_barrier(0);
+
+    Terms<T> terms[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float z[4][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = s[r][t][i];
+          if constexpr (is_coded(F)) x *= ks[t][i];
+          z[t][i] = x;
+        }
+      if (a.cap > 0.f) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z[t][i] = cap_log2 * squash<T>(z[t][i] * to_cap);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z[t][i] *= to_log2;
+      }
+      if (a.slopes) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z[t][i] = fmaf(-slope[r], fabsf((float)(pos[r] - kb - L::key_of(t, g, i))), z[t][i]);
+      }
+      if (masked) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!sees(a, wh, pos[r], kb + L::key_of(t, g, i))) z[t][i] = -kInf;
+      }
+      float top = z[0][0];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, z[t][i]);
+      top = over_groups(top, true);
+      const float m_new = fmaxf(m[r], top);
+      const float base = m_new == -kInf ? 0.f : m_new;
+      const float f = exp2_(m[r] - base);
+      m[r] = m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          z[t][i] = exp2_(z[t][i] - base);
+          sum += z[t][i];
+        }
+      l[r] = fmaf(l[r], f, sum);
+#pragma unroll
+      for (int c = 0; c < L::CT; ++c) o[r][c] *= f;
+      if constexpr (is_coded(F)) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            z[t][i] *= vs[t][i];
+            if (masked && !sees(a, wh, pos[r], kb + L::key_of(t, g, i))) z[t][i] = 0.f;
+          }
+      }
+      terms[r].set(z);
+    }
+    if (masked) {
+      // What a row does not see must not reach it: 0 times a NaN or infinity is
+      // NaN.  Finite values are multiplied as usual; the others are counted by
+      // a product of ones and added as infinities (both signs make a NaN).
+      const bool bad = clear_tail<F, DH>(vr, g, wh.ctx - kb);
+      if constexpr (F != EVO_CACHE_INT8) {
+        if (__any(bad)) {
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            float ones[4][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) ones[t][i] = sees(a, wh, pos[r], kb + L::key_of(t, g, i)) ? 1.f : 0.f;
+            Terms<T> seen;
+            seen.set(ones);
+#pragma unroll
+            for (int c = 0; c < L::CT; ++c)
+#pragma unroll
+              for (int which = 1; which <= 2; ++which) {
+                uint32_t x[L::VW];
+#pragma unroll
+                for (int e = 0; e < L::VW; ++e) x[e] = only<F>(vr[c][e], which);
+                const f32x4 n = value_tile<F>(x, seen, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (n[e] > 0.f) o[r][c][e] += which == 1 ? kInf : -kInf;
+              }
+          }
+#pragma unroll
+          for (int c = 0; c < L::CT; ++c)
+#pragma unroll
+            for (int e = 0; e < L::VW; ++e) vr[c][e] = only<F>(vr[c][e], 0);
+        }
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < L::CT; ++c)
+#pragma unroll
+      for (int r = 0; r < R; ++r) o[r][c] = value_tile<F>(vr[c], terms[r], o[r][c]);
+    __builtin_amdgcn_sched_barrier(0);
+    if (next >= 0) load_values(next);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  // ---- the four waves' results, in the order (w0 + w2) + (w1 + w3) ----
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    l[r] = over_groups(l[r], false);
+    if (g == 0) {
+      join_ml[w][r * 16 + lr][0] = m[r];
+      join_ml[w][r * 16 + lr][1] = l[r];
+    }
+  }
+  __syncthreads();
+  float total[R], top[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float M = -kInf;
+    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, join_ml[i][r * 16 + lr][0]);
+    const float base = M == -kInf ? 0.f : M;
+    float t = 0.f;
+    for (int i = 0; i < kWaves; ++i) t += join_ml[i][r * 16 + lr][1] * exp2_(join_ml[i][r * 16 + lr][0] - base);
+    total[r] = t;
+    top[r] = M;
+    const float f = exp2_(m[r] - base);
+#pragma unroll
+    for (int c = 0; c < L::CT; ++c) o[r][c] *= f;
+  }
+  const auto put = [&](float* dst) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int c = 0; c < L::CT; ++c) *reinterpret_cast<f32x4*>(dst + ((r * L::CT + c) * 64 + lane) * 4) = o[r][c];
+  };
+  const auto add = [&](const float* src) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int c = 0; c < L::CT; ++c) o[r][c] += *reinterpret_cast<const f32x4*>(src + ((r * L::CT + c) * 64 + lane) * 4);
+  };
+  if (w >= 2) put(join_o[w - 2]);
+  __syncthreads();
+  if (w < 2) add(join_o[w]);
+  __syncthreads();
+  if (w == 1) put(join_o[1]);
+  __syncthreads();
+  if (w != 0) return;
+  add(join_o[1]);
+
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = wh.base + r * 16 + lr;
+    if (row >= wh.rows) continue;
+    if (a.n_split > 1) {
+      const int64_t part = ((int64_t)th * a.n_split + split) * TR + r * 16 + lr;
+      if (g == 0) {
+        a.part_ml[part * 2] = top[r];
+        a.part_ml[part * 2 + 1] = total[r];
+      }
+      if (v0 < v1) {
+#pragma unroll
+        for (int c = 0; c < L::CT; ++c) *reinterpret_cast<f32x4*>(a.part + part * DH + c * 16 + g * 4) = o[r][c];
+      }
+      continue;
+    }
+    const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+    const float inv = total[r] == 0.f ? 0.f : 1.f / total[r];
+    T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
+#pragma unroll
+    for (int c = 0; c < L::CT; ++c)
+      store4(dst + c * 16 + g * 4, a.wide, total[r] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[r][c] * inv);
+    if (a.lse && g == 0)
+      a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] =
+          total[r] == 0.f ? -kInf : (top[r] + __builtin_amdgcn_logf(total[r])) * kLn2;
+  }
+}
+
+// Joins the parts of a row tile, in order.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
+  const int th = blockIdx.x, h = th % a.cache.n_kv_heads, tile = th / a.cache.n_kv_heads;
+  int seq;
+  Where wh;
+  if (!find_tile(a, tile, tile_rows, &seq, &wh)) return;
+  for (int x = threadIdx.x; x < tile_rows * (DH / 4); x += 256) {
+    const int r = x / (DH / 4), c = x % (DH / 4) * 4, row = wh.base + r;
+    if (row >= wh.rows) break;
+    const int64_t part = (int64_t)th * a.n_split * tile_rows + r;
+    float M = -kInf;
+    for (int s = 0; s < a.n_split; ++s) M = fmaxf(M, a.part_ml[(part + (int64_t)s * tile_rows) * 2]);
+    const float base = M == -kInf ? 0.f : M;
+    float t = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.n_split; ++s) {
+      const int64_t at = part + (int64_t)s * tile_rows;
+      const float l = a.part_ml[at * 2 + 1], f = exp2_(a.part_ml[at * 2] - base);
+      if (l == 0.f) continue;  // (a part that saw nothing wrote no outputs)
+      t += l * f;
+      o += *reinterpret_cast<const f32x4*>(a.part + at * DH + c) * f;
+    }
+    const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+    T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
+    store4(dst + c, a.wide, t == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / t));
+    if (a.lse && c == 0)
+      a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = t == 0.f ? -kInf : (M + __builtin_amdgcn_logf(t)) * kLn2;
+  }
+}
+
+template <typename T, int F, int DH>
+hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
+  const int64_t blocks = (int64_t)p.n_tiles * a.cache.n_kv_heads;
+  if (p.tile_rows == 16)
+    hipLaunchKernelGGL((stream_kernel<T, F, DH, 1>), dim3(blocks * p.n_split), dim3(kWaves * 64), 0, stream, a);
+  else if constexpr (!(F == EVO_CACHE_FP32 && DH == 128))
+    hipLaunchKernelGGL((stream_kernel<T, F, DH, 2>), dim3(blocks * p.n_split), dim3(kWaves * 64), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.n_split == 1) return e;
+  hipLaunchKernelGGL((join_kernel<T, DH>), dim3(blocks), dim3(256), 0, stream, a, p.tile_rows);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_kv_heads, const RowsView& r,
+                       int max_length, int window, bool causal, int n_cu) {
+  AttPlan p = {};
+  const int group = n_heads / n_kv_heads;
+  const int64_t rows = (int64_t)r.max_rows * group;  // of one sequence and key/value head
+  // (two row blocks of a block of fp32 keys of 128 do not fit the registers)
+  p.tile_rows = rows <= 16 || (format == EVO_CACHE_FP32 && head_dim == 128) ? 16 : 32;
+  // row tiles: as many for every sequence, or packed by the rows before
+  const int64_t even = (rows + p.tile_rows - 1) / p.tile_rows;
+  const int64_t packed = (int64_t)r.n_rows * group / p.tile_rows + r.n_seqs;
+  if (!r.cu || even * r.n_seqs <= packed) {
+    p.tiles_per_seq = (int)even;
+    p.n_tiles = (int)(even * r.n_seqs);
+  } else {
+    p.n_tiles = (int)packed;
+  }
+  const int64_t blocks = ((int64_t)max_length + kKeys - 1) / kKeys;
+  // parts: two workgroups for every compute unit, each with a block for every wave
+  const int64_t wgs = (int64_t)p.n_tiles * n_kv_heads;
+  const int64_t want = wgs ? (2 * (int64_t)n_cu + wgs - 1) / wgs : 1;
+  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, blocks / kWaves));
+  if (p.n_split > 1) {
+    p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
+    p.part_floats = wgs * p.n_split * p.tile_rows * head_dim;
+  }
+  return p;
+}
+
+hipError_t launch_attention(int dtype, int format, int head_dim, const AttPlan& plan, const AttArgs& a,
+                            hipStream_t stream) {
+#define X(D, T, F, DH) \
+  if (dtype == D && format == F && head_dim == DH) return launch_as<T, F, DH>(plan, a, stream);
+#define Y(DH)                             \
+  X(EVO_FP32, float, EVO_CACHE_FP32, DH)  \
+  X(EVO_FP32, float, EVO_CACHE_INT8, DH)  \
+  X(EVO_FP32, float, EVO_CACHE_FP8, DH)   \
+  X(EVO_BF16, __bf16, EVO_CACHE_BF16, DH) \
+  X(EVO_BF16, __bf16, EVO_CACHE_INT8, DH) \
+  X(EVO_BF16, __bf16, EVO_CACHE_FP8, DH)
+  Y(32) Y(64) Y(128)
+#undef Y
+#undef X
+  return hipErrorInvalidValue;
+}
+
+}  // namespace evo

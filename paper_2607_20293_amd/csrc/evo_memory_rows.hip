@@ -1,0 +1,444 @@
+// Rows of queries, keys and values around the paged cache: norm for each head
+// and rotation by position in one pass, quantising as the cache is written,
+// and reading it back.
+//
+// What bounds it: memory.  Every value is read once and written once; norm,
+// rotation and quantising are a few operations a value.
+//  * Queries and keys: a row of head_dim values lies over head_dim / 8 lanes,
+//    8 values a lane (16 bytes of bf16), so that the row's sum of squares or
+//    maximum takes 2 to 4 lane exchanges.  A group of lanes keeps its token's
+//    (cos, sin) and works through several heads, because the table's 8 bytes
+//    a pair would otherwise be four times the row's own traffic.
+//  * Values go to a transposed page: a lane takes a whole row (its maximum
+//    then needs no exchange) and a wave 64 consecutive tokens, so that each of
+//    the head_dim stores of a wave is a run of neighbouring slots.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "evo.h"
+#include "evo_memory.hpp"
+
+namespace evo {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kNone = -1;
+constexpr int kThreads = 256;
+
+template <int F> struct Held;
+template <> struct Held<EVO_CACHE_FP32> { typedef float type; };
+template <> struct Held<EVO_CACHE_BF16> { typedef __bf16 type; };
+template <> struct Held<EVO_CACHE_INT8> { typedef int8_t type; };
+template <> struct Held<EVO_CACHE_FP8> { typedef uint8_t type; };
+template <> struct Held<kNone> { typedef uint8_t type; };
+
+constexpr bool is_coded(int f) { return f == EVO_CACHE_INT8 || f == EVO_CACHE_FP8; }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ float low(uint32_t v) { return __builtin_bit_cast(float, v << 16); }
+__device__ __forceinline__ float high(uint32_t v) { return __builtin_bit_cast(float, v & 0xffff0000u); }
+
+// 8 consecutive values
+__device__ __forceinline__ void load8(const float* p, int wide, float* x) {
+  if (wide) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = p[e];
+  }
+}
+__device__ __forceinline__ void load8(const __bf16* p, int wide, float* x) {
+  if (wide) {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[2 * e] = low(a[e]); x[2 * e + 1] = high(a[e]); }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)p[e];
+  }
+}
+__device__ __forceinline__ void store8(float* p, int wide, const float* x) {
+  if (wide) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = x[e];
+  }
+}
+__device__ __forceinline__ void store8(__bf16* p, int wide, const float* x) {
+  if (wide) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = (__bf16)x[e];
+  }
+}
+
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+
+// How a row whose largest magnitude has the bits `top` is coded: code =
+// round(x / s).  The quotient comes from s's reciprocal and one residual step,
+// which gives the correctly rounded x / s, so that ties (frequent with bf16
+// inputs) fall as the definition says.  Rows near the smallest floats are
+// lifted first (lift), to keep the reciprocal finite.
+struct Coding {
+  float s, r, d, lift;
+};
+template <int F> __device__ __forceinline__ Coding coding_of(uint32_t top) {
+  constexpr float M = F == EVO_CACHE_INT8 ? 127.f : 448.f;
+  const float amax = __builtin_bit_cast(float, top);
+  Coding c;
+  if (top >= 0x7f800000u) {  // a NaN or an infinity in the row
+    c.s = __builtin_nanf("");
+    c.r = c.d = c.lift = 0.f;
+    return c;
+  }
+  c.s = amax / M;
+  c.lift = amax < 0x1p-60f ? 0x1p64f : 1.f;
+  c.d = c.s * c.lift;
+  c.r = c.d > 0.f ? 1.f / c.d : 0.f;
+  return c;
+}
+template <int F> __device__ __forceinline__ float quotient(float x, const Coding& c) {
+  constexpr float M = F == EVO_CACHE_INT8 ? 127.f : 448.f;
+  if (c.r == 0.f) return 0.f;
+  x *= c.lift;
+  const float q = x * c.r;
+  return __builtin_amdgcn_fmed3f(fmaf(fmaf(-q, c.d, x), c.r, q), -M, M);
+}
+// four codes, the first in the lowest byte
+template <int F> __device__ __forceinline__ uint32_t code4(const float* y) {
+  if (F == EVO_CACHE_FP8) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], v, true);
+  }
+  uint32_t v = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v |= ((uint32_t)(int)rintf(y[e]) & 0xffu) << (8 * e);
+  return v;
+}
+template <int F> __device__ __forceinline__ void decode4(uint32_t v, float* y) {
+  if (F == EVO_CACHE_FP8) {
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(v, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(v, true);
+    y[0] = a[0]; y[1] = a[1]; y[2] = b[0]; y[3] = b[1];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (float)(int8_t)(v >> (8 * e));
+  }
+}
+
+// Slot of position `pos` of a sequence: index of its (page, head) block, or -1
+// where there is none.
+__device__ __forceinline__ int64_t block_of(const RowsArgs& a, int seq, int pos, int head) {
+  if (pos < 0 || (pos >> a.cache.page_shift) >= a.rows.max_pages) return -1;
+  return (int64_t)page_of(a.rows, a.cache, seq, pos >> a.cache.page_shift) * a.cache.n_kv_heads + head;
+}
+
+// 8 consecutive keys of a cache row
+template <int F> __device__ __forceinline__ void store_key(const RowsArgs& a, int64_t at, int lane, const float* y,
+                                                            const Coding& c) {
+  typedef typename Held<F>::type H;
+  H* p = reinterpret_cast<H*>(a.cache.k) + at + lane * 8;
+  if constexpr (is_coded(F)) {
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = quotient<F>(y[e], c);
+    *reinterpret_cast<u32x2*>(p) = u32x2{code4<F>(z), code4<F>(z + 4)};
+  } else if constexpr (F != kNone) {
+    store8(p, 1, y);
+  }
+}
+
+template <typename T, int F, int DH>
+__device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
+  constexpr int LPR = DH / 8;  // lanes a row
+  const int heads = a.n_heads + a.n_kv_heads;
+  const int groups = (heads + a.heads_per_group - 1) / a.heads_per_group;  // groups of lanes a token
+  const int lane = threadIdx.x % LPR;
+  const int64_t g = ((int64_t)block * kThreads + threadIdx.x) / LPR;
+  // whole waves stay for the exchanges; rows past the end repeat the last one
+  // and are not stored
+  const int64_t tok = g / groups;
+  const bool live = tok < a.rows.n_rows;
+  const int n = live ? (int)tok : a.rows.n_rows - 1, h0 = (int)(g - tok * groups);
+  int seq = 0, i = 0, pos = 0;
+  if constexpr (F != kNone) {
+    find_row(a.rows, n, &seq, &i);
+    pos = a.starts[seq] + i;
+  }
+  const int turn = a.positions ? a.positions[n] : pos;
+  float cs[8], sn[8];
+  bool rotated = false;
+  if (a.half) {
+    // halves: the lane's 8 values meet pairs 8 lane' .. + 7; adjacent: 4 pairs
+    const bool in = turn >= 0 && turn < a.n_positions;
+    const float* t = a.table + (int64_t)(in ? turn : 0) * (2 * a.half);
+    rotated = lane * 8 < 2 * a.half;
+    if (rotated) {
+      if (a.adjacent) {
+        const f32x4 u = *reinterpret_cast<const f32x4*>(t + lane * 8), w = *reinterpret_cast<const f32x4*>(t + lane * 8 + 4);
+        cs[0] = cs[1] = u[0]; cs[2] = cs[3] = u[2]; cs[4] = cs[5] = w[0]; cs[6] = cs[7] = w[2];
+        sn[0] = -u[1]; sn[1] = u[1]; sn[2] = -u[3]; sn[3] = u[3];
+        sn[4] = -w[1]; sn[5] = w[1]; sn[6] = -w[3]; sn[7] = w[3];
+      } else {
+        const bool second = lane * 8 >= a.half;
+        const float* tt = t + 2 * (lane * 8 - (second ? a.half : 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 u = *reinterpret_cast<const f32x4*>(tt + 4 * e);
+          cs[2 * e] = u[0]; cs[2 * e + 1] = u[2];
+          sn[2 * e] = second ? u[1] : -u[1];
+          sn[2 * e + 1] = second ? u[3] : -u[3];
+        }
+      }
+    }
+    if (!in) {
+      rotated = true;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) cs[e] = sn[e] = __builtin_nanf("");
+    }
+  }
+  float qg[8], kg[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    qg[e] = a.norm && a.q_gain ? a.q_gain[lane * 8 + e] : 1.f;
+    kg[e] = a.norm && a.k_gain ? a.k_gain[lane * 8 + e] : 1.f;
+  }
+  const int half_lanes = a.half / 8;
+  const int partner = (threadIdx.x & 63) + (lane < half_lanes ? half_lanes : lane < 2 * half_lanes ? -half_lanes : 0);
+  for (int h = h0; h < heads; h += groups) {
+    const bool is_q = h < a.n_heads;
+    const int hk = h - a.n_heads;
+    const T* src = is_q ? reinterpret_cast<const T*>(a.q.p) + n * a.q.row + h * a.q.head
+                        : reinterpret_cast<const T*>(a.k.p) + n * a.k.row + hk * a.k.head;
+    float x[8];
+    load8(src + lane * 8, a.wide, x);
+    if (a.norm) {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+      for (int d = 1; d < LPR; d *= 2) ss += __shfl_xor(ss, d);
+      const float r = 1.f / sqrtf(ss * (1.f / DH) + a.eps);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = x[e] * r * (is_q ? qg[e] : kg[e]);
+    }
+    if (a.half) {
+      float o[8];
+      if (a.adjacent) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = x[e ^ 1];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = __shfl(x[e], partner);
+      }
+      if (rotated) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(o[e], sn[e], x[e] * cs[e]);
+      }
+    }
+    if (is_q || F == kNone) {
+      T* dst = is_q ? reinterpret_cast<T*>(a.qo.p) + n * a.qo.row + h * a.qo.head
+                    : reinterpret_cast<T*>(a.ko.p) + n * a.ko.row + hk * a.ko.head;
+      if (live) store8(dst + lane * 8, a.wide, x);
+      continue;
+    }
+    Coding c = {};
+    if constexpr (is_coded(F)) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, magnitude(x[e]));
+#pragma unroll
+      for (int d = 1; d < LPR; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+      c = coding_of<F>(top);
+    }
+    const int64_t b = block_of(a, seq, pos, hk);
+    if (live && b >= 0) {
+      const int64_t row = (b << a.cache.page_shift) + (pos & ((1 << a.cache.page_shift) - 1));
+      store_key<F>(a, row * DH, lane, x, c);
+      if (is_coded(F) && lane == 0) a.cache.ks[row] = c.s;
+    }
+  }
+}
+
+template <typename T, int F, int DH>
+__device__ __forceinline__ void v_rows(const RowsArgs& a, int block) {
+  typedef typename Held<F>::type H;
+  const int w = block * (kThreads / 64) + (int)(threadIdx.x >> 6);
+  const int h = w % a.n_kv_heads;
+  const int64_t n = (int64_t)(w / a.n_kv_heads) * 64 + (threadIdx.x & 63);
+  if (n >= a.rows.n_rows) return;
+  int seq, i;
+  find_row(a.rows, (int)n, &seq, &i);
+  const int pos = a.starts[seq] + i;
+  const int64_t b = block_of(a, seq, pos, h);
+  if (b < 0) return;
+  const int slot = pos & ((1 << a.cache.page_shift) - 1);
+  const T* src = reinterpret_cast<const T*>(a.v.p) + n * a.v.row + h * a.v.head;
+  float x[DH];
+#pragma unroll
+  for (int c = 0; c < DH; c += 8) load8(src + c, a.wide, x + c);
+  H* dst = reinterpret_cast<H*>(a.cache.v) + ((b * DH) << a.cache.page_shift) + slot;
+  if constexpr (is_coded(F)) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 0; c < DH; ++c) top = max(top, magnitude(x[c]));
+    const Coding cd = coding_of<F>(top);
+    a.cache.vs[(b << a.cache.page_shift) + slot] = cd.s;
+#pragma unroll
+    for (int c = 0; c < DH; c += 4) {
+      float z[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[e] = quotient<F>(x[c + e], cd);
+      const uint32_t v = code4<F>(z);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dst[(int64_t)(c + e) << a.cache.page_shift] = (H)(v >> (8 * e));
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < DH; ++c) dst[(int64_t)c << a.cache.page_shift] = (H)x[c];
+  }
+}
+
+template <typename T, int F, int DH>
+__global__ void __launch_bounds__(kThreads) rows_kernel(RowsArgs a) {
+  if ((int)blockIdx.x < a.qk_blocks) qk_rows<T, F, DH>(a, blockIdx.x);
+  else if constexpr (F != kNone) v_rows<T, F, DH>(a, blockIdx.x - a.qk_blocks);
+}
+
+// ---- reading back: keys a group of lanes a row, values a lane a row --------
+template <typename T, int F, int DH>
+__global__ void __launch_bounds__(kThreads) read_kernel(RowsArgs a) {
+  typedef typename Held<F>::type H;
+  const int ps = a.cache.page_shift;
+  if ((int)blockIdx.x < a.qk_blocks) {
+    constexpr int LPR = DH / 8;
+    const int lane = threadIdx.x % LPR;
+    const int64_t g = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / LPR;
+    const int64_t n = g / a.n_kv_heads;
+    const int h = (int)(g - n * a.n_kv_heads);
+    if (n >= a.rows.n_rows) return;
+    int seq, i;
+    find_row(a.rows, (int)n, &seq, &i);
+    const int pos = a.starts[seq] + i;
+    const int64_t b = block_of(a, seq, pos, h);
+    float x[8] = {};
+    if (b >= 0) {
+      const int64_t row = (b << ps) + (pos & ((1 << ps) - 1));
+      const H* p = reinterpret_cast<const H*>(a.cache.k) + row * DH + lane * 8;
+      if constexpr (is_coded(F)) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+        const float s = a.cache.ks[row];
+        decode4<F>(v[0], x);
+        decode4<F>(v[1], x + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= s;
+      } else {
+        load8(p, 1, x);
+      }
+    }
+    store8(reinterpret_cast<T*>(a.ko.p) + n * a.ko.row + h * a.ko.head + lane * 8, a.wide, x);
+    return;
+  }
+  const int w = (blockIdx.x - a.qk_blocks) * (kThreads / 64) + (int)(threadIdx.x >> 6);
+  const int h = w % a.n_kv_heads;
+  const int64_t n = (int64_t)(w / a.n_kv_heads) * 64 + (threadIdx.x & 63);
+  if (n >= a.rows.n_rows) return;
+  int seq, i;
+  find_row(a.rows, (int)n, &seq, &i);
+  const int pos = a.starts[seq] + i;
+  const int64_t b = block_of(a, seq, pos, h);
+  const int slot = pos & ((1 << ps) - 1);
+  const H* p = reinterpret_cast<const H*>(a.cache.v) + ((b * DH) << ps) + slot;
+  T* dst = reinterpret_cast<T*>(a.v.p) + n * a.v.row + h * a.v.head;
+  float s = 1.f;
+  if constexpr (is_coded(F)) s = b >= 0 ? a.cache.vs[(b << ps) + slot] : 0.f;
+#pragma unroll
+  for (int c = 0; c < DH; c += 8) {
+    float x[8] = {};
+    if (b >= 0) {
+      if constexpr (is_coded(F)) {
+        uint32_t v[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e / 4] |= (uint32_t)(uint8_t)p[(int64_t)(c + e) << ps] << (8 * (e & 3));
+        decode4<F>(v[0], x);
+        decode4<F>(v[1], x + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= s;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)p[(int64_t)(c + e) << ps];
+      }
+    }
+    store8(dst + c, a.wide, x);
+  }
+}
+
+int v_blocks(const RowsArgs& a) {
+  const int64_t waves = ((int64_t)a.rows.n_rows + 63) / 64 * a.n_kv_heads;
+  return (int)((waves + kThreads / 64 - 1) / (kThreads / 64));
+}
+
+template <typename T, int F, int DH>
+hipError_t launch_rows_as(RowsArgs a, hipStream_t stream) {
+  constexpr int LPR = DH / 8;
+  const int heads = a.n_heads + a.n_kv_heads;
+  a.heads_per_group = 1;
+  const int groups = (heads + a.heads_per_group - 1) / a.heads_per_group;
+  a.qk_blocks = (int)(((int64_t)a.rows.n_rows * groups * LPR + kThreads - 1) / kThreads);
+  hipLaunchKernelGGL((rows_kernel<T, F, DH>), dim3(a.qk_blocks + (F == kNone ? 0 : v_blocks(a))), dim3(kThreads), 0,
+                     stream, a);
+  return hipGetLastError();
+}
+
+template <typename T, int F, int DH>
+hipError_t launch_read_as(RowsArgs a, hipStream_t stream) {
+  constexpr int LPR = DH / 8;
+  a.qk_blocks = (int)(((int64_t)a.rows.n_rows * a.n_kv_heads * LPR + kThreads - 1) / kThreads);
+  hipLaunchKernelGGL((read_kernel<T, F, DH>), dim3(a.qk_blocks + v_blocks(a)), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+#define EVO_ROW_TYPES(X, DH)      \
+  X(EVO_FP32, float, EVO_CACHE_FP32, DH)  \
+  X(EVO_FP32, float, EVO_CACHE_INT8, DH)  \
+  X(EVO_FP32, float, EVO_CACHE_FP8, DH)   \
+  X(EVO_BF16, __bf16, EVO_CACHE_BF16, DH) \
+  X(EVO_BF16, __bf16, EVO_CACHE_INT8, DH) \
+  X(EVO_BF16, __bf16, EVO_CACHE_FP8, DH)
+
+}  // namespace
+
+hipError_t launch_rows(int dtype, int format, int head_dim, RowsArgs a, hipStream_t stream) {
+#define X(D, T, F, DH) \
+  if (dtype == D && format == F && head_dim == DH) return launch_rows_as<T, F, DH>(a, stream);
+#define Y(DH)                                   \
+  EVO_ROW_TYPES(X, DH)                          \
+  X(EVO_FP32, float, kNone, DH)                 \
+  X(EVO_BF16, __bf16, kNone, DH)
+  Y(32) Y(64) Y(128)
+#undef Y
+#undef X
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_cache_read(int dtype, int format, int head_dim, RowsArgs a, hipStream_t stream) {
+#define X(D, T, F, DH) \
+  if (dtype == D && format == F && head_dim == DH) return launch_read_as<T, F, DH>(a, stream);
+  EVO_ROW_TYPES(X, 32) EVO_ROW_TYPES(X, 64) EVO_ROW_TYPES(X, 128)
+#undef X
+  return hipErrorInvalidValue;
+}
+
+}  // namespace evo

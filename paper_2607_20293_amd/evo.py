@@ -28,7 +28,8 @@ EXPORTED = ("evo_weight_count", "evo_check_desc", "evo_create_policy", "evo_set_
             "evo_guided_sample", "evo_ga_initial_population", "evo_ga_next_generation", "evo_ga_search",
             "evo_search", "evo_encoder_weight_count", "evo_create_encoder", "evo_encode", "evo_encoder_flops",
             "evo_destroy_encoder", "evo_set_kernel_timing", "evo_kernel_time", "evo_denoise_noalloc",
-            "evo_noalloc_scratch_bytes", "evo_debug_encoder_plan")
+            "evo_noalloc_scratch_bytes", "evo_debug_encoder_plan", "evo_qk_norm_rope", "evo_cache_write",
+            "evo_cache_read", "evo_qkv_write", "evo_chunk_attention", "evo_chunk_attention_workspace")
 
 
 def guided_probabilities(scores, eps: float, gamma: float) -> np.ndarray:
@@ -266,6 +267,19 @@ def lib() -> ctypes.CDLL:
         L.evo_debug_encoder_plan.restype = ctypes.c_int
         L.evo_destroy_encoder.argtypes = [P]
         L.evo_destroy_encoder.restype = None
+        C, R, N, H, A = (ctypes.POINTER(x) for x in (KVCacheDesc, KVRows, NormRope, Heads, Attention))
+        L.evo_qk_norm_rope.argtypes = [N, I32, I32, I32, I32, I32, H, H, P, H, H, P]
+        L.evo_qk_norm_rope.restype = ctypes.c_int
+        L.evo_cache_write.argtypes = [C, R, I32, P, H, H, P]
+        L.evo_cache_write.restype = ctypes.c_int
+        L.evo_cache_read.argtypes = [C, R, I32, P, H, H, P]
+        L.evo_cache_read.restype = ctypes.c_int
+        L.evo_qkv_write.argtypes = [C, R, N, I32, I32, P, H, H, H, H, P]
+        L.evo_qkv_write.restype = ctypes.c_int
+        L.evo_chunk_attention_workspace.argtypes = [C, R, A]
+        L.evo_chunk_attention_workspace.restype = ctypes.c_int64
+        L.evo_chunk_attention.argtypes = [C, R, A, H, H, P, P, ctypes.c_size_t, P]
+        L.evo_chunk_attention.restype = ctypes.c_int
         L.evo_last_error.argtypes = []
         L.evo_last_error.restype = ctypes.c_char_p
         _lib = L
@@ -590,3 +604,313 @@ class Encoder:
         v = ctypes.c_uint64()
         _check(lib().evo_encoder_flops(self._h, batch, ctypes.byref(v)))
         return int(v.value)
+
+
+# --------------------------------------------------------------------------
+# long memories: norm and rotation, the paged cache, attention over it
+# --------------------------------------------------------------------------
+class KVCacheDesc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("format", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class KVRows(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("cu_rows", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class NormRope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("n_positions", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p),
+                ("table", ctypes.c_void_p)]
+
+
+class Attention(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("max_length", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("cap", ctypes.c_float), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("prefix", ctypes.c_void_p), ("slopes", ctypes.c_void_p)]
+
+
+CACHE_FP32, CACHE_BF16, CACHE_INT8, CACHE_FP8 = 0, 1, 2, 3
+_PAIRS = {"halves": 0, "adjacent": 1}
+_ref = ctypes.byref
+
+
+def _row_dtype(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return EVO_BF16
+    if t.dtype == torch.float32:
+        return EVO_FP32
+    raise TypeError(f"expected float32 or bfloat16 rows, got {t.dtype}")
+
+
+def _heads(name, t, dtype, rows, heads, dh, device) -> Heads:
+    """A [rows][heads][dh] tensor with any row and head strides."""
+    if t.dtype != dtype or t.device != device:
+        raise TypeError(f"{name}: expected {dtype} on {device}, got {t.dtype} on {t.device}")
+    if t.shape != (rows, heads, dh):
+        raise ValueError(f"{name}: expected shape {(rows, heads, dh)}, got {tuple(t.shape)}")
+    s = t.stride()
+    if s[2] != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return Heads(t.data_ptr(), s[0], s[1])
+
+
+def _ints(name, t, shape, device) -> int:
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.device != device:
+        raise TypeError(f"{name}: expected an int32 tensor on {device}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _floats(name, t, shape, device):
+    import torch
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.device != device:
+        raise TypeError(f"{name}: expected a float32 tensor on {device}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _device_of(t):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("expected a HIP device tensor")
+    return t.device
+
+
+class _On:
+    """The stream of a call: the caller's, or the device's current one.  Makes
+    the device current; tensors allocated here for a stream that is not the
+    current one are kept until its work is done."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.device, self.given = device, stream
+        self.current = torch.cuda.current_stream(device)
+        self.stream = self.current if stream is None else stream
+        self.other = None
+        if torch.cuda.current_device() != device.index:
+            self.other = torch.cuda.device(device)
+            self.other.__enter__()
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+    @property
+    def handle(self):
+        return self.stream.cuda_stream
+
+    def empty(self, shape, dtype):
+        import torch
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if self.given is not None and self.given != self.current:
+            t.record_stream(self.given)
+        return t
+
+
+def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, device="cuda"):
+    """(cos, sin) of position * theta^(-2i / rotary_dim), float32
+    [n_positions][rotary_dim / 2][2], computed in 64 bits."""
+    import torch
+    inv = theta ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64, device=device) / rotary_dim)
+    a = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * inv
+    return torch.stack([a.cos(), a.sin()], dim=-1).float().contiguous()
+
+
+class KVCache:
+    """A paged cache of keys and values around the caller's tensors (see
+    evo_kv_cache in include/evo.h):
+      k [pages][heads][page_size][dh], v [pages][heads][dh][page_size]
+    of float32, bfloat16, int8 or float8_e4m3fn; 8-bit caches also have
+    k_scale and v_scale, float32 [pages][heads][page_size]."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        device = _device_of(k)
+        formats = {torch.float32: CACHE_FP32, torch.bfloat16: CACHE_BF16, torch.int8: CACHE_INT8,
+                   torch.float8_e4m3fn: CACHE_FP8}
+        if k.dtype not in formats:
+            raise TypeError(f"no cache format holds {k.dtype}")
+        if k.dim() != 4 or v.dtype != k.dtype or v.device != device:
+            raise ValueError("k must be [pages][heads][page_size][dh], v of its type on its device")
+        pages, heads, size, dh = k.shape
+        if v.shape != (pages, heads, dh, size) or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("v must be [pages][heads][dh][page_size], and both contiguous")
+        fmt = formats[k.dtype]
+        if (fmt >= CACHE_INT8) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise ValueError("8-bit caches have scales, the others have none")
+        ks, vs = (_floats(n, t, (pages, heads, size), device) for n, t in (("k_scale", k_scale), ("v_scale", v_scale)))
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, device
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pages, heads, size, dh
+        self.desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), ks, vs, fmt, pages, size, heads, dh)
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 64, dtype=None, device="cuda"):
+        """An unwritten cache of its own tensors (dtype: bfloat16 by default)."""
+        import torch
+        dtype = torch.bfloat16 if dtype is None else dtype
+        k = torch.empty((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
+        v = torch.empty((n_pages, n_kv_heads, head_dim, page_size), dtype=dtype, device=device)
+        if dtype not in (torch.int8, torch.float8_e4m3fn):
+            return cls(k, v)
+        return cls(k, v, *(torch.empty((n_pages, n_kv_heads, page_size), device=device) for _ in range(2)))
+
+    def rows(self, page_table, n_rows: int, cu_rows, max_rows) -> KVRows:
+        """The rows of a call (evo_kv_rows): page_table int32 [seqs][pages];
+        cu_rows int32 [seqs + 1] or None (as many rows in every sequence)."""
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [sequences][pages]")
+        seqs, wide = page_table.shape
+        if cu_rows is None:
+            if seqs == 0 or n_rows % seqs:
+                raise ValueError(f"{n_rows} rows over {seqs} sequences need cu_rows")
+            max_rows = n_rows // seqs
+        elif max_rows is None:
+            max_rows = n_rows
+        return KVRows(seqs, n_rows, max_rows, wide,
+                      None if cu_rows is None else _ints("cu_rows", cu_rows, (seqs + 1,), self.device),
+                      _ints("page_table", page_table, (seqs, wide), self.device))
+
+
+def _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device) -> NormRope:
+    if pairs not in _PAIRS:
+        raise ValueError("pairs must be 'halves' or 'adjacent'")
+    rotary = n_positions = 0
+    if table is not None:
+        if table.dim() != 3:
+            raise ValueError("table must be [positions][rotary_dim / 2][2]")
+        n_positions, rotary = table.shape[0], 2 * table.shape[1]
+        _floats("table", table, (n_positions, rotary // 2, 2), device)
+    return NormRope(rotary, _PAIRS[pairs], n_positions, -1.0 if eps is None else eps,
+                    _floats("q_gain", q_gain, (dh,), device), _floats("k_gain", k_gain, (dh,), device),
+                    None if table is None else table.data_ptr())
+
+
+def qk_norm_rope(q, k, positions, table, q_gain=None, k_gain=None, eps: Optional[float] = 1e-6, pairs: str = "halves",
+                 out=None, stream=None):
+    """evo_qk_norm_rope: q [rows][heads][dh] and k [rows][kv_heads][dh]
+    (float32 or bfloat16, any row and head strides) normalised for each head
+    (eps None: not) and rotated by positions (int32 [rows]) with the table
+    (float32 [n_positions][rotary_dim / 2][2]; None: not).  out: (q_out,
+    k_out), which may be (q, k).  Returns (q_out, k_out)."""
+    device = _device_of(q)
+    dt = _row_dtype(q)
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [rows][heads][dh]")
+    n, hq, dh = q.shape
+    hk = k.shape[1]
+    nr = _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device)
+    with _On(device, stream) as on:
+        q_out, k_out = (on.empty((n, hq, dh), q.dtype), on.empty((n, hk, dh), q.dtype)) if out is None else out
+        _check(lib().evo_qk_norm_rope(
+            _ref(nr), dt, dh, n, hq, hk, _ref(_heads("q", q, q.dtype, n, hq, dh, device)),
+            _ref(_heads("k", k, q.dtype, n, hk, dh, device)),
+            None if table is None else _ints("positions", positions, (n,), device),
+            _ref(_heads("q_out", q_out, q.dtype, n, hq, dh, device)),
+            _ref(_heads("k_out", k_out, q.dtype, n, hk, dh, device)), on.handle))
+    return q_out, k_out
+
+
+def cache_write(cache: KVCache, page_table, starts, k, v, cu_rows=None, max_rows: Optional[int] = None, stream=None):
+    """evo_cache_write: k, v [rows][kv_heads][dh] into the cache, row i of
+    sequence s at position starts[s] + i (int32 [sequences])."""
+    n, dh, device = k.shape[0], cache.head_dim, cache.device
+    dt = _row_dtype(k)
+    rows = cache.rows(page_table, n, cu_rows, max_rows)
+    with _On(device, stream) as on:
+        _check(lib().evo_cache_write(
+            _ref(cache.desc), _ref(rows), dt, _ints("starts", starts, (rows.n_seqs,), device),
+            _ref(_heads("k", k, k.dtype, n, cache.n_kv_heads, dh, device)),
+            _ref(_heads("v", v, k.dtype, n, cache.n_kv_heads, dh, device)), on.handle))
+
+
+def cache_read(cache: KVCache, page_table, starts, n_rows: int, dtype, cu_rows=None, max_rows: Optional[int] = None,
+               out=None, stream=None):
+    """evo_cache_read: positions starts[s] + i of every sequence as (k, v),
+    [n_rows][kv_heads][dh] of dtype."""
+    dh, device = cache.head_dim, cache.device
+    rows = cache.rows(page_table, n_rows, cu_rows, max_rows)
+    with _On(device, stream) as on:
+        shape = (n_rows, cache.n_kv_heads, dh)
+        k, v = (on.empty(shape, dtype), on.empty(shape, dtype)) if out is None else out
+        _check(lib().evo_cache_read(
+            _ref(cache.desc), _ref(rows), _row_dtype(k), _ints("starts", starts, (rows.n_seqs,), device),
+            _ref(_heads("k_out", k, dtype, *shape, device)), _ref(_heads("v_out", v, dtype, *shape, device)), on.handle))
+    return k, v
+
+
+def qkv_write(cache: KVCache, page_table, starts, q, k, v, table, q_gain=None, k_gain=None,
+              eps: Optional[float] = 1e-6, pairs: str = "halves", cu_rows=None, max_rows: Optional[int] = None,
+              q_out=None, stream=None):
+    """evo_qkv_write: q normalised and rotated into q_out (returned), k
+    normalised, rotated and written, v written; rotation by the positions
+    starts[s] + i that are written."""
+    device, dh = cache.device, cache.head_dim
+    dt = _row_dtype(q)
+    if q.dim() != 3:
+        raise ValueError("q must be [rows][heads][dh]")
+    n, hq = q.shape[0], q.shape[1]
+    rows = cache.rows(page_table, n, cu_rows, max_rows)
+    nr = _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device)
+    with _On(device, stream) as on:
+        q_out = on.empty((n, hq, dh), q.dtype) if q_out is None else q_out
+        _check(lib().evo_qkv_write(
+            _ref(cache.desc), _ref(rows), _ref(nr), dt, hq, _ints("starts", starts, (rows.n_seqs,), device),
+            _ref(_heads("q", q, q.dtype, n, hq, dh, device)),
+            _ref(_heads("k", k, q.dtype, n, cache.n_kv_heads, dh, device)),
+            _ref(_heads("v", v, q.dtype, n, cache.n_kv_heads, dh, device)),
+            _ref(_heads("q_out", q_out, q.dtype, n, hq, dh, device)), on.handle))
+    return q_out
+
+
+def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_rows: Optional[int] = None, *,
+                    scale: Optional[float] = None, causal: bool = False, window: int = 0, cap: float = 0.0,
+                    slopes=None, prefix=None, starts=None, max_length: int = 0, out=None, lse=None, stream=None):
+    """evo_chunk_attention: q [rows][heads][dh] over the cache's positions
+    0 .. lengths[s] - 1 (int32 [sequences]).  scale: 1 / sqrt(dh) by default;
+    prefix, starts: int32 [sequences] or None (starts: lengths - rows);
+    slopes: float32 [heads] or None; max_length: a bound of lengths, for the
+    plan alone (0: the page table's).  Returns (out [rows][heads][dh], lse
+    float32 [rows][heads])."""
+    import torch
+    device, dh = cache.device, cache.head_dim
+    dt = _row_dtype(q)
+    if q.dim() != 3:
+        raise ValueError("q must be [rows][heads][dh]")
+    n, hq = q.shape[0], q.shape[1]
+    rows = cache.rows(page_table, n, cu_rows, max_rows)
+    seqs = (rows.n_seqs,)
+    att = Attention(dt, hq, 1 if causal else 0, window, max_length, dh ** -0.5 if scale is None else scale, cap,
+                    _ints("lengths", lengths, seqs, device),
+                    None if starts is None else _ints("starts", starts, seqs, device),
+                    None if prefix is None else _ints("prefix", prefix, seqs, device),
+                    _floats("slopes", slopes, (hq,), device))
+    L = lib()
+    with _On(device, stream) as on:
+        out = on.empty((n, hq, dh), q.dtype) if out is None else out
+        lse = on.empty((n, hq), torch.float32) if lse is None else lse
+        need = L.evo_chunk_attention_workspace(_ref(cache.desc), _ref(rows), _ref(att))
+        if need < 0:
+            _check(int(need))
+        work = on.empty((need,), torch.uint8) if need else None
+        _check(L.evo_chunk_attention(
+            _ref(cache.desc), _ref(rows), _ref(att), _ref(_heads("q", q, q.dtype, n, hq, dh, device)),
+            _ref(_heads("out", out, q.dtype, n, hq, dh, device)), _floats("lse", lse, (n, hq), device),
+            None if work is None else work.data_ptr(), need, on.handle))
+    return out, lse
