@@ -35,7 +35,7 @@ struct HeadsView {
 struct RowsArgs {
   HeadsView q, k, v, qo, ko;  // ko: keys that do not go to the cache
   int n_heads, n_kv_heads;
-  int heads_per_group;        // heads that a group of lanes works through
+  int head_groups;            // workgroups that share a token's heads
   int norm, half, adjacent, n_positions;
   float eps;
   const float* q_gain;

@@ -28,6 +28,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kNone = -1;
 constexpr int kThreads = 256;
+constexpr int kAhead = 4;     // heads whose rows a lane requests ahead
+constexpr int kFill = 2048;   // workgroups that fill the device (8 a compute unit)
 
 template <int F> struct Held;
 template <> struct Held<EVO_CACHE_FP32> { typedef float type; };
@@ -160,18 +162,47 @@ template <int F> __device__ __forceinline__ void store_key(const RowsArgs& a, in
   }
 }
 
+// A row's 8 values of a lane as they lie in memory.
+template <typename T> struct Raw { u32x4 w[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T* p, int wide) {
+  Raw<T> r;
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const u32x4*>(p)[i];
+  } else {
+    T* d = reinterpret_cast<T*>(&r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] = p[e];
+  }
+  return r;
+}
+__device__ __forceinline__ void unpack(const Raw<__bf16>& r, float* x) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { x[2 * e] = low(r.w[0][e]); x[2 * e + 1] = high(r.w[0][e]); }
+}
+__device__ __forceinline__ void unpack(const Raw<float>& r, float* x) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(float, (uint32_t)r.w[e / 4][e % 4]);
+}
+
 template <typename T, int F, int DH>
 __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
   constexpr int LPR = DH / 8;  // lanes a row
-  const int heads = a.n_heads + a.n_kv_heads;
-  const int groups = (heads + a.heads_per_group - 1) / a.heads_per_group;  // groups of lanes a token
+  const int heads = a.n_heads + a.n_kv_heads, groups = a.head_groups;
   const int lane = threadIdx.x % LPR;
-  const int64_t g = ((int64_t)block * kThreads + threadIdx.x) / LPR;
+  const int tok = (block / groups) * (kThreads / LPR) + (int)threadIdx.x / LPR, h0 = block % groups;
   // whole waves stay for the exchanges; rows past the end repeat the last one
   // and are not stored
-  const int64_t tok = g / groups;
   const bool live = tok < a.rows.n_rows;
-  const int n = live ? (int)tok : a.rows.n_rows - 1, h0 = (int)(g - tok * groups);
+  const int n = live ? tok : a.rows.n_rows - 1;
+  const auto source = [&](int h) {
+    return (h < a.n_heads ? reinterpret_cast<const T*>(a.q.p) + n * a.q.row + h * a.q.head
+                          : reinterpret_cast<const T*>(a.k.p) + n * a.k.row + (h - a.n_heads) * a.k.head) + lane * 8;
+  };
+  Raw<T> next[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    if (h0 + u * groups < heads) next[u] = load_raw(source(h0 + u * groups), a.wide);
   int seq = 0, i = 0, pos = 0;
   if constexpr (F != kNone) {
     find_row(a.rows, n, &seq, &i);
@@ -217,13 +248,12 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
   }
   const int half_lanes = a.half / 8;
   const int partner = (threadIdx.x & 63) + (lane < half_lanes ? half_lanes : lane < 2 * half_lanes ? -half_lanes : 0);
-  for (int h = h0; h < heads; h += groups) {
+
+  const auto one = [&](int h, const Raw<T>& raw) {
     const bool is_q = h < a.n_heads;
     const int hk = h - a.n_heads;
-    const T* src = is_q ? reinterpret_cast<const T*>(a.q.p) + n * a.q.row + h * a.q.head
-                        : reinterpret_cast<const T*>(a.k.p) + n * a.k.row + hk * a.k.head;
     float x[8];
-    load8(src + lane * 8, a.wide, x);
+    unpack(raw, x);
     if (a.norm) {
       float ss = 0.f;
 #pragma unroll
@@ -252,7 +282,7 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
       T* dst = is_q ? reinterpret_cast<T*>(a.qo.p) + n * a.qo.row + h * a.qo.head
                     : reinterpret_cast<T*>(a.ko.p) + n * a.ko.row + hk * a.ko.head;
       if (live) store8(dst + lane * 8, a.wide, x);
-      continue;
+      return;
     }
     Coding c = {};
     if constexpr (is_coded(F)) {
@@ -269,73 +299,171 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
       store_key<F>(a, row * DH, lane, x, c);
       if (is_coded(F) && lane == 0) a.cache.ks[row] = c.s;
     }
+  };
+  for (int h = h0; h < heads; h += kAhead * groups) {
+    Raw<T> now[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      now[u] = next[u];
+      const int hn = h + (kAhead + u) * groups;
+      if (hn < heads) next[u] = load_raw(source(hn), a.wide);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (h + u * groups < heads) one(h + u * groups, now[u]);
   }
 }
 
-template <typename T, int F, int DH>
-__device__ __forceinline__ void v_rows(const RowsArgs& a, int block) {
-  typedef typename Held<F>::type H;
+// A wave's 64 rows of values pass through LDS a slice of kSlice bytes at a time,
+// because a lane that reads (or writes) a row of its own touches a cache line 16
+// bytes at a time: staged, P lanes take a row's part of a slice, RP rows at once.
+constexpr int kSlice = 128, kPitch = kSlice + 16;
+template <typename T, int DH> struct Slices {
+  static constexpr int N = kSlice / (int)sizeof(T);
+  static constexpr int V = N < DH ? N : DH;            // values of a row in a slice
+  static constexpr int P = V * (int)sizeof(T) / 16;
+  static constexpr int RP = 64 / P;
+  static constexpr int C = DH / V;                     // slices
+};
+// the address that lane r holds
+__device__ __forceinline__ char* address_of(char* p, int r) {
+  const uint64_t u = (uint64_t)p;
+  const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)u, r), hi = (uint32_t)__shfl((int)(uint32_t)(u >> 32), r);
+  return reinterpret_cast<char*>(lo | (uint64_t)hi << 32);
+}
+// LDS that one wave writes and reads: its accesses are in order, the compiler
+// has to keep them so
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+__device__ __forceinline__ uint32_t top_of(u32x4 w, __bf16) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m = max(m, max((w[e] << 16) & 0x7fffffffu, w[e] & 0x7fff0000u));
+  return m;
+}
+__device__ __forceinline__ uint32_t top_of(u32x4 w, float) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m = max(m, w[e] & 0x7fffffffu);
+  return m;
+}
+
+// The wave's 64 rows of values and where they lie: lane l has row l.
+struct ValueRow {
+  int n, h, slot;
+  int64_t block;  // -1: the row has no slot
+  bool live;
+};
+__device__ __forceinline__ ValueRow value_row(const RowsArgs& a, int block) {
   const int w = block * (kThreads / 64) + (int)(threadIdx.x >> 6);
-  const int h = w % a.n_kv_heads;
+  ValueRow r;
+  r.h = w % a.n_kv_heads;
   const int64_t n = (int64_t)(w / a.n_kv_heads) * 64 + (threadIdx.x & 63);
-  if (n >= a.rows.n_rows) return;
+  r.live = n < a.rows.n_rows;
+  r.n = r.live ? (int)n : a.rows.n_rows - 1;
   int seq, i;
-  find_row(a.rows, (int)n, &seq, &i);
+  find_row(a.rows, r.n, &seq, &i);
   const int pos = a.starts[seq] + i;
-  const int64_t b = block_of(a, seq, pos, h);
-  if (b < 0) return;
-  const int slot = pos & ((1 << a.cache.page_shift) - 1);
-  const T* src = reinterpret_cast<const T*>(a.v.p) + n * a.v.row + h * a.v.head;
-  float x[DH];
+  r.block = block_of(a, seq, pos, r.h);
+  r.slot = pos & ((1 << a.cache.page_shift) - 1);
+  return r;
+}
+
+template <typename T, int F, int DH>
+__device__ __forceinline__ void v_rows(const RowsArgs& a, int block, char* lds, uint32_t* tops) {
+  typedef typename Held<F>::type H;
+  typedef Slices<T, DH> S;
+  const int lane = threadIdx.x & 63;
+  const ValueRow r = value_row(a, block);
+  const bool live = r.live && r.block >= 0;
+  char* src = a.v.p + (r.n * a.v.row + r.h * a.v.head) * (int64_t)sizeof(T);
+  u32x4 w[S::C][S::P];
 #pragma unroll
-  for (int c = 0; c < DH; c += 8) load8(src + c, a.wide, x + c);
-  H* dst = reinterpret_cast<H*>(a.cache.v) + ((b * DH) << a.cache.page_shift) + slot;
-  if constexpr (is_coded(F)) {
-    uint32_t top = 0;
+  for (int i = 0; i < S::P; ++i) {
+    const char* p = address_of(src, i * S::RP + lane / S::P) + (lane % S::P) * 16;
 #pragma unroll
-    for (int c = 0; c < DH; ++c) top = max(top, magnitude(x[c]));
-    const Coding cd = coding_of<F>(top);
-    a.cache.vs[(b << a.cache.page_shift) + slot] = cd.s;
+    for (int c = 0; c < S::C; ++c) {
+      if (a.wide) {
+        w[c][i] = *reinterpret_cast<const u32x4*>(p + c * kSlice);
+      } else {
+        T* d = reinterpret_cast<T*>(&w[c][i]);
 #pragma unroll
-    for (int c = 0; c < DH; c += 4) {
-      float z[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[e] = quotient<F>(x[c + e], cd);
-      const uint32_t v = code4<F>(z);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) dst[(int64_t)(c + e) << a.cache.page_shift] = (H)(v >> (8 * e));
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) d[e] = reinterpret_cast<const T*>(p + c * kSlice)[e];
+      }
     }
-  } else {
+  }
+  Coding cd = {};
+  if constexpr (is_coded(F)) {
 #pragma unroll
-    for (int c = 0; c < DH; ++c) dst[(int64_t)c << a.cache.page_shift] = (H)x[c];
+    for (int i = 0; i < S::P; ++i) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int c = 0; c < S::C; ++c) m = max(m, top_of(w[c][i], T()));
+#pragma unroll
+      for (int d = 1; d < S::P; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+      if (lane % S::P == 0) tops[i * S::RP + lane / S::P] = m;
+    }
+    wave_sync();
+    cd = coding_of<F>(tops[lane]);
+    if (live) a.cache.vs[(r.block << a.cache.page_shift) + r.slot] = cd.s;
+  }
+  H* dst = reinterpret_cast<H*>(a.cache.v) + ((r.block * DH) << a.cache.page_shift) + r.slot;
+#pragma unroll
+  for (int c = 0; c < S::C; ++c) {
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < S::P; ++i)
+      *reinterpret_cast<u32x4*>(lds + (i * S::RP + lane / S::P) * kPitch + (lane % S::P) * 16) = w[c][i];
+    wave_sync();
+    if (live) {
+#pragma unroll
+      for (int j = 0; j < S::V; j += 8) {
+        float x[8];
+        load8(reinterpret_cast<const T*>(lds + lane * kPitch) + j, 1, x);
+        if constexpr (is_coded(F)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = quotient<F>(x[e], cd);
+          const uint32_t v[2] = {code4<F>(x), code4<F>(x + 4)};
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            dst[(int64_t)(c * S::V + j + e) << a.cache.page_shift] = (H)(v[e / 4] >> (8 * (e & 3)));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dst[(int64_t)(c * S::V + j + e) << a.cache.page_shift] = (H)x[e];
+        }
+      }
+    }
   }
 }
 
 template <typename T, int F, int DH>
 __global__ void __launch_bounds__(kThreads) rows_kernel(RowsArgs a) {
+  __shared__ __attribute__((aligned(16))) char stage[F == kNone ? 1 : kThreads / 64][F == kNone ? 16 : 64 * kPitch];
+  __shared__ uint32_t tops[F == kNone ? 1 : kThreads];
+  const int w = threadIdx.x >> 6;
   if ((int)blockIdx.x < a.qk_blocks) qk_rows<T, F, DH>(a, blockIdx.x);
-  else if constexpr (F != kNone) v_rows<T, F, DH>(a, blockIdx.x - a.qk_blocks);
+  else if constexpr (F != kNone) v_rows<T, F, DH>(a, blockIdx.x - a.qk_blocks, stage[w], tops + w * 64);
 }
 
-// ---- reading back: keys a group of lanes a row, values a lane a row --------
+// ---- reading back: keys a group of lanes a token, values a lane a row ------
 template <typename T, int F, int DH>
-__global__ void __launch_bounds__(kThreads) read_kernel(RowsArgs a) {
+__device__ __forceinline__ void read_keys(const RowsArgs& a, int block) {
   typedef typename Held<F>::type H;
-  const int ps = a.cache.page_shift;
-  if ((int)blockIdx.x < a.qk_blocks) {
-    constexpr int LPR = DH / 8;
-    const int lane = threadIdx.x % LPR;
-    const int64_t g = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / LPR;
-    const int64_t n = g / a.n_kv_heads;
-    const int h = (int)(g - n * a.n_kv_heads);
-    if (n >= a.rows.n_rows) return;
-    int seq, i;
-    find_row(a.rows, (int)n, &seq, &i);
-    const int pos = a.starts[seq] + i;
-    const int64_t b = block_of(a, seq, pos, h);
+  constexpr int LPR = DH / 8;
+  const int ps = a.cache.page_shift, groups = a.head_groups;
+  const int lane = threadIdx.x % LPR;
+  const int n = (block / groups) * (kThreads / LPR) + (int)threadIdx.x / LPR;
+  if (n >= a.rows.n_rows) return;
+  int seq, i;
+  find_row(a.rows, n, &seq, &i);
+  const int pos = a.starts[seq] + i;
+  const int64_t b = block_of(a, seq, pos, 0);
+  for (int h = block % groups; h < a.n_kv_heads; h += groups) {
     float x[8] = {};
     if (b >= 0) {
-      const int64_t row = (b << ps) + (pos & ((1 << ps) - 1));
+      const int64_t row = ((b + h) << ps) + (pos & ((1 << ps) - 1));
       const H* p = reinterpret_cast<const H*>(a.cache.k) + row * DH + lane * 8;
       if constexpr (is_coded(F)) {
         const u32x2 v = *reinterpret_cast<const u32x2*>(p);
@@ -349,40 +477,66 @@ __global__ void __launch_bounds__(kThreads) read_kernel(RowsArgs a) {
       }
     }
     store8(reinterpret_cast<T*>(a.ko.p) + n * a.ko.row + h * a.ko.head + lane * 8, a.wide, x);
-    return;
   }
-  const int w = (blockIdx.x - a.qk_blocks) * (kThreads / 64) + (int)(threadIdx.x >> 6);
-  const int h = w % a.n_kv_heads;
-  const int64_t n = (int64_t)(w / a.n_kv_heads) * 64 + (threadIdx.x & 63);
-  if (n >= a.rows.n_rows) return;
-  int seq, i;
-  find_row(a.rows, (int)n, &seq, &i);
-  const int pos = a.starts[seq] + i;
-  const int64_t b = block_of(a, seq, pos, h);
-  const int slot = pos & ((1 << ps) - 1);
-  const H* p = reinterpret_cast<const H*>(a.cache.v) + ((b * DH) << ps) + slot;
-  T* dst = reinterpret_cast<T*>(a.v.p) + n * a.v.row + h * a.v.head;
-  float s = 1.f;
-  if constexpr (is_coded(F)) s = b >= 0 ? a.cache.vs[(b << ps) + slot] : 0.f;
+}
+
+template <typename T, int F, int DH>
+__device__ __forceinline__ void read_values(const RowsArgs& a, int block, char* lds) {
+  typedef typename Held<F>::type H;
+  typedef Slices<T, DH> S;
+  const int ps = a.cache.page_shift, lane = threadIdx.x & 63;
+  const ValueRow r = value_row(a, block);
+  const uint64_t rows = __ballot(r.live);
+  char* dst = a.v.p + (r.n * a.v.row + r.h * a.v.head) * (int64_t)sizeof(T);
+  const H* src = reinterpret_cast<const H*>(a.cache.v) + ((r.block * DH) << ps) + r.slot;
+  float s = 0.f;
+  if constexpr (is_coded(F)) s = r.block >= 0 ? a.cache.vs[(r.block << ps) + r.slot] : 0.f;
 #pragma unroll
-  for (int c = 0; c < DH; c += 8) {
-    float x[8] = {};
-    if (b >= 0) {
-      if constexpr (is_coded(F)) {
-        uint32_t v[2] = {0, 0};
+  for (int c = 0; c < S::C; ++c) {
+    wave_sync();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e / 4] |= (uint32_t)(uint8_t)p[(int64_t)(c + e) << ps] << (8 * (e & 3));
-        decode4<F>(v[0], x);
-        decode4<F>(v[1], x + 4);
+    for (int j = 0; j < S::V; j += 8) {
+      float x[8] = {};
+      if (r.block >= 0) {
+        const H* p = src + ((int64_t)(c * S::V + j) << ps);
+        if constexpr (is_coded(F)) {
+          uint32_t v[2] = {0, 0};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= s;
+          for (int e = 0; e < 8; ++e) v[e / 4] |= (uint32_t)(uint8_t)p[(int64_t)e << ps] << (8 * (e & 3));
+          decode4<F>(v[0], x);
+          decode4<F>(v[1], x + 4);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= s;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = (float)p[(int64_t)e << ps];
+        }
+      }
+      store8(reinterpret_cast<T*>(lds + lane * kPitch) + j, 1, x);
+    }
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < S::P; ++i) {
+      const int row = i * S::RP + lane / S::P;
+      const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * kPitch + (lane % S::P) * 16);
+      char* p = address_of(dst, row) + c * kSlice + (lane % S::P) * 16;
+      if (!(rows >> row & 1)) continue;
+      if (a.wide) {
+        *reinterpret_cast<u32x4*>(p) = w;
       } else {
+        const T* d = reinterpret_cast<const T*>(&w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)p[(int64_t)(c + e) << ps];
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) reinterpret_cast<T*>(p)[e] = d[e];
       }
     }
-    store8(dst + c, a.wide, x);
   }
+}
+
+template <typename T, int F, int DH>
+__global__ void __launch_bounds__(kThreads) read_kernel(RowsArgs a) {
+  __shared__ __attribute__((aligned(16))) char stage[kThreads / 64][64 * kPitch];
+  if ((int)blockIdx.x < a.qk_blocks) read_keys<T, F, DH>(a, blockIdx.x);
+  else read_values<T, F, DH>(a, blockIdx.x - a.qk_blocks, stage[threadIdx.x >> 6]);
 }
 
 int v_blocks(const RowsArgs& a) {
@@ -390,13 +544,18 @@ int v_blocks(const RowsArgs& a) {
   return (int)((waves + kThreads / 64 - 1) / (kThreads / 64));
 }
 
+// Workgroups of the part that takes a token's heads in turn: as few groups of
+// heads as still fill the device.
+template <int DH> void spread_heads(RowsArgs* a, int heads) {
+  constexpr int per = kThreads / (DH / 8);  // tokens of a workgroup
+  const int64_t blocks = ((int64_t)a->rows.n_rows + per - 1) / per;
+  a->head_groups = (int)std::max<int64_t>(1, std::min<int64_t>(heads, (kFill + blocks - 1) / blocks));
+  a->qk_blocks = (int)(blocks * a->head_groups);
+}
+
 template <typename T, int F, int DH>
 hipError_t launch_rows_as(RowsArgs a, hipStream_t stream) {
-  constexpr int LPR = DH / 8;
-  const int heads = a.n_heads + a.n_kv_heads;
-  a.heads_per_group = 1;
-  const int groups = (heads + a.heads_per_group - 1) / a.heads_per_group;
-  a.qk_blocks = (int)(((int64_t)a.rows.n_rows * groups * LPR + kThreads - 1) / kThreads);
+  spread_heads<DH>(&a, a.n_heads + a.n_kv_heads);
   hipLaunchKernelGGL((rows_kernel<T, F, DH>), dim3(a.qk_blocks + (F == kNone ? 0 : v_blocks(a))), dim3(kThreads), 0,
                      stream, a);
   return hipGetLastError();
@@ -404,8 +563,7 @@ hipError_t launch_rows_as(RowsArgs a, hipStream_t stream) {
 
 template <typename T, int F, int DH>
 hipError_t launch_read_as(RowsArgs a, hipStream_t stream) {
-  constexpr int LPR = DH / 8;
-  a.qk_blocks = (int)(((int64_t)a.rows.n_rows * a.n_kv_heads * LPR + kThreads - 1) / kThreads);
+  spread_heads<DH>(&a, a.n_kv_heads);
   hipLaunchKernelGGL((read_kernel<T, F, DH>), dim3(a.qk_blocks + v_blocks(a)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
