@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(kWaves * 64) stream_kernel(AttArgs a) {
       // a product of ones and added as infinities (both signs make a NaN).
       const bool bad = clear_tail<F, DH>(vr, g, wh.ctx - kb);
       if constexpr (F != EVO_CACHE_INT8) {
-        if (__any(bad)) {
+        if (__builtin_expect(__any(bad), 0)) {
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             float ones[4][4];
@@ -650,6 +650,359 @@ __global__ void __launch_bounds__(kWaves * 64) stream_kernel(AttArgs a) {
   }
 }
 
+// ---- long chunks ------------------------------------------------------------
+// A workgroup takes 32 rows a wave and shares its keys and values through LDS:
+// with hundreds of rows to a key/value head the products are the cost, and a
+// block's 64 keys are read from memory once for all waves.  Same transposed
+// products, with 32x32 matrix instructions.
+//  * LDS holds two blocks as bf16 (codes converted on the way); the next block
+//    waits in registers while this one is multiplied, one barrier a block.
+//  * 16-byte chunks of an LDS row are exchanged by the row's number (key_turn,
+//    channel & 7), so that the 8 lanes of a read's phase meet 8 bank groups.
+//  * The maximum moves only when a row's scores outgrow it by 2^8: terms stay
+//    below 2^8 of the true maximum's, and the outputs are seldom rescaled.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// The LDS row of a block's key that matrix row r of a 32-key tile takes: bits 2
+// and 3 exchanged, which leaves a lane with runs of 8 keys.
+__device__ __forceinline__ int key_row(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
+__device__ __forceinline__ int key_turn(int key) { return (key & 3) | ((key >> 1) & 4); }
+
+__device__ __forceinline__ float other_half(float x, bool maximum) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const float a0 = __builtin_bit_cast(float, (uint32_t)a[0]), a1 = __builtin_bit_cast(float, (uint32_t)a[1]);
+  return maximum ? fmaxf(a0, a1) : a0 + a1;
+}
+
+// One block on its way from memory to LDS.
+template <int F, int DH, int NW> struct Stage {
+  static constexpr int SZ = size_of(F), TH = NW * 64;
+  static constexpr int KC = kKeys * DH * SZ / 16;       // 16-byte chunks of keys, as many of values
+  static constexpr int IT = (2 * KC + TH - 1) / TH;
+  static constexpr int KROW = DH * SZ / 16, VROW = kKeys * SZ / 16;
+  static constexpr int KB = kKeys * DH * 2, BYTES = 2 * KB;
+  u32x4 w[IT];
+  float scale;
+
+  // the block's keys and values start at kp and vp, value rows 1 << ps slots apart
+  __device__ __forceinline__ void load(const char* kp, const char* vp, int ps, const float* ks, const float* vs) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int c = i * TH + (int)threadIdx.x;
+      if (2 * KC % TH && c >= 2 * KC) break;
+      if (c < KC) w[i] = *reinterpret_cast<const u32x4*>(kp + c * 16);
+      else w[i] = *reinterpret_cast<const u32x4*>(vp + ((size_t)(uint32_t)((c - KC) / VROW) << ps) * SZ + (c - KC) % VROW * 16);
+    }
+    if constexpr (is_coded(F)) scale = threadIdx.x < 128 ? (threadIdx.x < 64 ? ks : vs - 64)[threadIdx.x] : 0.f;
+  }
+  // left: keys of the block that the cache holds; values past it become 0.
+  // check: some row does not see all of the block; NaNs and infinities among
+  // its values become 0 then, and *bad is set.
+  __device__ __forceinline__ void store(char* lds, float* scales, int left, bool check, int* bad) const {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int c = i * TH + (int)threadIdx.x;
+      if (2 * KC % TH && c >= 2 * KC) break;
+      u32x4 x = w[i];
+      if (c >= KC && left < kKeys) {
+        const int key = (c - KC) % VROW * (16 / SZ);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int e = 0; e < 4 / SZ; ++e)
+            if (key + d * (4 / SZ) + e >= left) x[d] &= ~(((1u << (8 * SZ)) - 1) << (8 * SZ * e));
+      }
+      if constexpr (F != EVO_CACHE_INT8) {
+        if (check && c >= KC) {
+          bool found = false;
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const uint32_t y = only<F>(x[d], 0);
+            found |= y != x[d];
+            x[d] = y;
+          }
+          if (found) *bad = 1;
+        }
+      }
+      char* row;
+      int at, turn;
+      if (c < KC) {
+        const int key = c / KROW;
+        row = lds + key * (DH * 2);
+        at = c % KROW * (2 / SZ);
+        turn = key_turn(key) & (DH / 8 - 1);
+      } else {
+        const int ch = (c - KC) / VROW;
+        row = lds + KB + ch * (kKeys * 2);
+        at = (c - KC) % VROW * (2 / SZ);
+        turn = ch & 7;
+      }
+      if constexpr (is_coded(F)) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const u32x2 lo = codes_bf16<F>(x[2 * b]), hi = codes_bf16<F>(x[2 * b + 1]);
+          *reinterpret_cast<u32x4*>(row + ((at + b) ^ turn) * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+        }
+      } else {
+        *reinterpret_cast<u32x4*>(row + (at ^ turn) * 16) = x;
+      }
+    }
+    if constexpr (is_coded(F))
+      if (threadIdx.x < 128) scales[threadIdx.x] = scale;
+  }
+};
+
+// Workgroup (row tile of 32 NW rows, key/value head, part of the keys).
+template <int F, int DH, int NW>
+__global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
+  typedef Stage<F, DH, NW> S;
+  constexpr int TR = 32 * NW, CT = DH / 32;
+  __shared__ __attribute__((aligned(16))) char stage[2][S::BYTES];
+  __shared__ __attribute__((aligned(16))) float scales[is_coded(F) ? 2 : 1][is_coded(F) ? 128 : 1];
+  __shared__ int bad[4];  // of block v at v & 3: cleared two blocks ahead, so that a barrier lies on either side
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 31, half = lane >> 5;
+  // heads fastest, so that a head's row tiles meet on few dies and share their
+  // caches; then the parts; the last row tiles, which see most, first
+  const int h = blockIdx.x % a.cache.n_kv_heads, rest = blockIdx.x / a.cache.n_kv_heads;
+  const int split = rest % a.n_split, tile = a.n_tiles - 1 - rest / a.n_split;
+  int seq;
+  Where wh;
+  if (!find_tile(a, tile, TR, &seq, &wh)) return;
+  const Blocks bl = blocks_of(a, wh);
+  const int per = max((bl.count + a.n_split - 1) / a.n_split, 1);
+  const int v0 = min(split * per, bl.count), v1 = min(v0 + per, bl.count);
+  const int ps = a.cache.page_shift;
+
+  const int row = min(wh.base + w * 32 + lr, wh.rows - 1), tok = row / a.group, head = h * a.group + row - tok * a.group;
+  const int pos = wh.start + tok;
+  const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+  // what this wave's rows see, to skip masks and whole blocks
+  Where ww = wh;
+  {
+    const int r0 = wh.base + w * 32;
+    ww.p_first = wh.start + min(r0, wh.rows - 1) / a.group;
+    ww.p_last = wh.start + min(r0 + 31, wh.rows - 1) / a.group;
+  }
+  // scores in units of log2: with no cap or bias by one factor inside the
+  // exponential (its sign moved to the query, so that the largest product is
+  // the largest score), else ahead of it
+  const bool plain = a.cap == 0.f && !a.slopes && a.scale != 0.f;
+  const float factor = plain ? fabsf(a.scale) * kLog2e : 1.f;
+  const float to_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, cap_log2 = a.cap * kLog2e, to_log2 = a.scale * kLog2e;
+  bf16x8 q[DH / 16];
+  {
+    const __bf16* p = reinterpret_cast<const __bf16*>(a.q.p) + (wh.row0 + tok) * a.q.row + head * a.q.head + half * 8;
+    const uint32_t flip = plain && a.scale < 0.f ? 0x80008000u : 0;
+#pragma unroll
+    for (int k = 0; k < DH / 16; ++k) {
+      if (a.wide) q[k] = *reinterpret_cast<const bf16x8*>(p + k * 16);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[k][e] = p[k * 16 + e];
+      u32x4 x = __builtin_bit_cast(u32x4, q[k]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] ^= flip;
+      q[k] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  f32x16 o[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
+  float m = -kInf, l = 0.f;
+
+  const int krow = key_row(lr) * (DH * 2), kturn = (key_turn(key_row(lr)) & (DH / 8 - 1)) ^ half;
+  const int vrow = S::KB + lr * (kKeys * 2), vturn = (lr & 7) ^ half;
+  S next;
+  const auto fetch = [&](int kb) {
+    const int slot = kb & ((1 << ps) - 1);
+    const int64_t b = (int64_t)page_of(a.rows, a.cache, seq, kb >> ps) * a.cache.n_kv_heads + h;
+    next.load(reinterpret_cast<const char*>(a.cache.k) + ((b << ps) + slot) * (DH * S::SZ),
+              reinterpret_cast<const char*>(a.cache.v) + (((b * DH) << ps) + slot) * S::SZ, ps,
+              is_coded(F) ? a.cache.ks + (b << ps) + slot : nullptr, is_coded(F) ? a.cache.vs + (b << ps) + slot : nullptr);
+  };
+  const auto put = [&](int v, int slot) {
+    const int kb = bl.at(v) * kKeys;
+    next.store(stage[slot], scales[is_coded(F) ? slot : 0], wh.ctx - kb, !sees_all(a, wh, kb), &bad[v & 3]);
+  };
+  if (v0 < v1) {
+    fetch(bl.at(v0) * kKeys);
+    if (threadIdx.x < 4) bad[threadIdx.x] = 0;
+    __syncthreads();
+    put(v0, 0);
+  }
+  for (int v = v0; v < v1; ++v) {
+    const int kb = bl.at(v) * kKeys, slot = (v - v0) & 1;
+    const char* lds = stage[slot];
+    __syncthreads();  // this block lies in LDS, and the block before is done with
+    if (threadIdx.x == 0) bad[(v + 2) & 3] = 0;
+    if (v + 1 < v1) fetch(bl.at(v + 1) * kKeys);
+    const bool any = kb < ww.prefix || ((!a.causal || kb <= ww.p_last) &&
+                     (!a.window || (kb < ww.p_last + a.window && kb + kKeys > ww.p_first - a.window + 1)));
+    if (any) {
+      const bool masked = !sees_all(a, ww, kb);
+      f32x16 s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < DH / 16; ++k)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bf16x8 x = *reinterpret_cast<const bf16x8*>(lds + krow + t * (32 * DH * 2) + (((2 * k) ^ kturn) * 16));
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[k], s[t], 0, 0, 0);
+        }
+      // element e of tile t is key 32 t + 16 (e / 8) + 8 half + e % 8
+      const auto key_at = [&](int t, int e) { return kb + 32 * t + 16 * (e >> 3) + 8 * half + (e & 7); };
+      if constexpr (is_coded(F)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(&scales[slot][32 * t + 16 * (e >> 3) + 8 * half + (e & 7)]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[t][e + i] *= x[i];
+          }
+      }
+      if (!plain) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            float z = s[t][e];
+            z = a.cap > 0.f ? cap_log2 * squash<__bf16>(z * to_cap) : z * to_log2;
+            if (a.slopes) z = fmaf(-slope, fabsf((float)(pos - key_at(t, e))), z);
+            s[t][e] = z;
+          }
+      }
+      if (masked) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!sees(a, wh, pos, key_at(t, e))) s[t][e] = -kInf;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+      top = other_half(top, true) * factor;
+      if (__any(!(top <= m + 8.f))) {
+        const float m_new = fmaxf(m, top);
+        const float f = exp2_(m - (m_new == -kInf ? 0.f : m_new));
+        m = m_new;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[c][e] *= f;
+      }
+      const float base = m == -kInf ? 0.f : m;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[t][e] = exp2_(fmaf(s[t][e], factor, -base));
+          sum += s[t][e];
+        }
+      l += sum;
+      if constexpr (is_coded(F)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(&scales[slot][64 + 32 * t + 16 * (e >> 3) + 8 * half + (e & 7)]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[t][e + i] *= x[i];
+          }
+        if (masked) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (!sees(a, wh, pos, key_at(t, e))) s[t][e] = 0.f;
+        }
+      }
+      bf16x8 p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        u32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = pack2(s[j >> 1][(j & 1) * 8 + 2 * e], s[j >> 1][(j & 1) * 8 + 2 * e + 1]);
+        p[j] = __builtin_bit_cast(bf16x8, x);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          const bf16x8 x = *reinterpret_cast<const bf16x8*>(lds + vrow + c * (32 * kKeys * 2) + (((2 * j) ^ vturn) * 16));
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[j], o[c], 0, 0, 0);
+        }
+      if constexpr (F != EVO_CACHE_INT8) {
+        if (__builtin_expect(bad[v & 3], 0)) {
+          // the values that store() took out, for the rows that see them
+          const int s0 = kb & ((1 << ps) - 1);
+          const int64_t b = (int64_t)page_of(a.rows, a.cache, seq, kb >> ps) * a.cache.n_kv_heads + h;
+#pragma unroll 1
+          for (int j = 0; j < min(kKeys, wh.ctx - kb); ++j) {
+            const bool see = sees(a, wh, pos, kb + j);
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const int64_t at = ((b * DH + c * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) << ps) + s0 + j;
+                uint32_t x;
+                if constexpr (F == EVO_CACHE_FP8) {
+                  x = reinterpret_cast<const uint8_t*>(a.cache.v)[at];
+                  x = (x & 0x7f) == 0x7f ? 0x7fc00000u : 0;
+                } else {
+                  x = (uint32_t)reinterpret_cast<const uint16_t*>(a.cache.v)[at] << 16;
+                }
+                if (see && (x & 0x7f800000u) == 0x7f800000u) o[c][e] += __builtin_bit_cast(float, x);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+          }
+        }
+      }
+    }
+    if (v + 1 < v1) put(v + 1, slot ^ 1);
+  }
+
+  l = other_half(l, false);
+  const int r = w * 32 + lr;
+  if (wh.base + r >= wh.rows) return;
+  if (a.n_split > 1) {
+    const int64_t part = (((int64_t)tile * a.cache.n_kv_heads + h) * a.n_split + split) * TR + r;
+    if (half == 0) {
+      a.part_ml[part * 2] = m;
+      a.part_ml[part * 2 + 1] = l;
+    }
+    if (v0 >= v1) return;
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<f32x4*>(a.part + part * DH + c * 32 + 2 * e + 4 * half) = f32x4{o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]};
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  __bf16* dst = reinterpret_cast<__bf16*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      store4(dst + c * 32 + 2 * e + 4 * half, a.wide,
+             l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]} * inv);
+  if (a.lse && half == 0)
+    a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 // Joins the parts of a row tile, in order.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
@@ -684,7 +1037,14 @@ __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
 template <typename T, int F, int DH>
 hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
   const int64_t blocks = (int64_t)p.n_tiles * a.cache.n_kv_heads;
-  if (p.tile_rows == 16)
+  if (p.tile_rows > 32) {
+    if constexpr (sizeof(T) == 2) {
+      if (p.tile_rows == 128)
+        hipLaunchKernelGGL((tile_kernel<F, DH, 4>), dim3(blocks * p.n_split), dim3(256), 0, stream, a);
+      else
+        hipLaunchKernelGGL((tile_kernel<F, DH, 8>), dim3(blocks * p.n_split), dim3(512), 0, stream, a);
+    }
+  } else if (p.tile_rows == 16)
     hipLaunchKernelGGL((stream_kernel<T, F, DH, 1>), dim3(blocks * p.n_split), dim3(kWaves * 64), 0, stream, a);
   else if constexpr (!(F == EVO_CACHE_FP32 && DH == 128))
     hipLaunchKernelGGL((stream_kernel<T, F, DH, 2>), dim3(blocks * p.n_split), dim3(kWaves * 64), 0, stream, a);
@@ -703,6 +1063,7 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   const int64_t rows = (int64_t)r.max_rows * group;  // of one sequence and key/value head
   // (two row blocks of a block of fp32 keys of 128 do not fit the registers)
   p.tile_rows = rows <= 16 || (format == EVO_CACHE_FP32 && head_dim == 128) ? 16 : 32;
+  if (dtype == EVO_BF16 && rows > 64) p.tile_rows = rows <= 128 ? 128 : 256;
   // row tiles: as many for every sequence, or packed by the rows before
   const int64_t even = (rows + p.tile_rows - 1) / p.tile_rows;
   const int64_t packed = (int64_t)r.n_rows * group / p.tile_rows + r.n_seqs;
@@ -715,7 +1076,7 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   const int64_t blocks = ((int64_t)max_length + kKeys - 1) / kKeys;
   // parts: two workgroups for every compute unit, each with a block for every wave
   const int64_t wgs = (int64_t)p.n_tiles * n_kv_heads;
-  const int64_t want = wgs ? (2 * (int64_t)n_cu + wgs - 1) / wgs : 1;
+  const int64_t want = wgs ? ((p.tile_rows == 256 ? 1 : 2) * (int64_t)n_cu + wgs - 1) / wgs : 1;
   p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, blocks / kWaves));
   if (p.n_split > 1) {
     p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
