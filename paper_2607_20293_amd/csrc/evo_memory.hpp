@@ -36,6 +36,7 @@ struct RowsArgs {
   HeadsView q, k, v, qo, ko;  // ko: keys that do not go to the cache
   int n_heads, n_kv_heads;
   int head_groups;            // workgroups that share a token's heads
+  int heads_by_rows;          // heads that go a group of lanes a row: q, k, and v of short calls
   int norm, half, adjacent, n_positions;
   float eps;
   const float* q_gain;

@@ -279,9 +279,33 @@ __device__ __forceinline__ f32x4 value_tile(const uint32_t* v, const Terms<float
   return o;
 }
 
-// What a masked block's values may hold where a row does not see them: keys
-// past the cache's length become 0 (a page's unused end may hold anything).
-// Returns, for formats that can hold them, whether a NaN or infinity is left.
+// Values that hold a NaN or an infinity set to 0 (int8 codes hold none; a cache
+// that was written holds no NaN codes of fp8, unwritten memory may).
+template <int F> __device__ __forceinline__ uint32_t finite_only(uint32_t x) {
+  if constexpr (F == EVO_CACHE_FP32) return (x & 0x7f800000u) == 0x7f800000u ? 0 : x;
+  if constexpr (F == EVO_CACHE_BF16) {
+    if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+    if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+  }
+  if constexpr (F == EVO_CACHE_FP8) {
+    // 0x80 in the bytes that are 0x7f or 0xff; times 255: the whole byte
+    const uint32_t nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    x &= ~((nan >> 7) * 255u);
+  }
+  return x;
+}
+// The value at an index if it is a NaN or an infinity, else 0.
+template <int F> __device__ __forceinline__ float not_finite(const void* v, int64_t at) {
+  uint32_t x;
+  if constexpr (F == EVO_CACHE_FP32) x = reinterpret_cast<const uint32_t*>(v)[at];
+  else if constexpr (F == EVO_CACHE_BF16) x = (uint32_t)reinterpret_cast<const uint16_t*>(v)[at] << 16;
+  else x = (reinterpret_cast<const uint8_t*>(v)[at] & 0x7f) == 0x7f ? 0x7fc00000u : 0;
+  return (x & 0x7f800000u) == 0x7f800000u ? __builtin_bit_cast(float, x) : 0.f;
+}
+
+// A masked block's values: keys past the cache's length become 0 (a page's
+// unused end may hold anything), NaNs and infinities too; returns whether
+// there were any.
 template <int F, int DH, int CT, int VW>
 __device__ __forceinline__ bool clear_tail(uint32_t (&v)[CT][VW], int g, int left) {
   typedef Lay<F, DH> L;
@@ -300,43 +324,14 @@ __device__ __forceinline__ bool clear_tail(uint32_t (&v)[CT][VW], int g, int lef
       for (int c = 0; c < L::CT; ++c) {
         uint32_t& x = v[c][l * 4 + d];
         x &= keep;
-        if constexpr (F == EVO_CACHE_FP32) bad |= (x & 0x7f800000u) == 0x7f800000u;
-        if constexpr (F == EVO_CACHE_BF16) bad |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-        if constexpr (F == EVO_CACHE_FP8) bad |= (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+        if constexpr (F != EVO_CACHE_INT8) {
+          const uint32_t y = finite_only<F>(x);
+          bad |= y != x;
+          x = y;
+        }
       }
     }
   return bad;
-}
-
-// v with its NaNs and infinities replaced: by 0 (which = 0), or 1 where it is
-// +infinity or NaN (which = 1), -infinity or NaN (which = 2) and 0 elsewhere.
-// (A cache that was written holds no NaN codes; unwritten memory may.)
-template <int F> __device__ __forceinline__ uint32_t only(uint32_t x, int which) {
-  if constexpr (F == EVO_CACHE_FP8) {
-    uint32_t r = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t y = (x >> (8 * e)) & 0xffu;
-      const bool nan = (y & 0x7fu) == 0x7fu;
-      r |= (which == 0 ? (nan ? 0 : y) : (nan ? 0x38u : 0)) << (8 * e);  // 0x38: 1
-    }
-    return r;
-  }
-  if constexpr (F == EVO_CACHE_FP32) {
-    const bool bad = (x & 0x7f800000u) == 0x7f800000u, nan = bad && (x & 0x7fffffu);
-    if (which == 0) return bad ? 0 : x;
-    return bad && (nan || (x >> 31) == (uint32_t)(which - 1)) ? 0x3f800000u : 0;
-  } else {
-    uint32_t r = 0;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t y = (x >> (16 * e)) & 0xffffu;
-      const bool bad = (y & 0x7f80u) == 0x7f80u, nan = bad && (y & 0x7fu);
-      const uint32_t z = which == 0 ? (bad ? 0 : y) : (bad && (nan || (y >> 15) == (uint32_t)(which - 1)) ? 0x3f80u : 0);
-      r |= z << (16 * e);
-    }
-    return r;
-  }
 }
 
 template <typename T> __device__ __forceinline__ void store4(T* p, int wide, f32x4 x) {
@@ -354,8 +349,13 @@ template <typename T> __device__ __forceinline__ void store4(T* p, int wide, f32
 }
 
 // Workgroup (row tile, key/value head, part of the keys).
+// Waves that a SIMD shall hold: what the registers of a wave's block allow.
+template <typename T> constexpr int waves_per_simd(int f, int dh, int r) {
+  return sizeof(T) == 4 || (dh == 128 && (f == EVO_CACHE_BF16 || r == 2)) ? 1 : r == 2 || dh == 128 ? 2 : 3;
+}
+
 template <typename T, int F, int DH, int R>
-__global__ void __launch_bounds__(kWaves * 64) stream_kernel(AttArgs a) {
+__global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stream_kernel(AttArgs a) {
   typedef Lay<F, DH> L;
   constexpr int TR = 16 * R;
   __shared__ __attribute__((aligned(16))) float join_o[2][TR * DH];
@@ -532,46 +532,40 @@ __global__ void __launch_bounds__(kWaves * 64) stream_kernel(AttArgs a) {
       }
       terms[r].set(z);
     }
+    bool bad = false;
     if (masked) {
-      // What a row does not see must not reach it: 0 times a NaN or infinity is
-      // NaN.  Finite values are multiplied as usual; the others are counted by
-      // a product of ones and added as infinities (both signs make a NaN).
-      const bool bad = clear_tail<F, DH>(vr, g, wh.ctx - kb);
-      if constexpr (F != EVO_CACHE_INT8) {
-        if (__builtin_expect(__any(bad), 0)) {
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            float ones[4][4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) ones[t][i] = sees(a, wh, pos[r], kb + L::key_of(t, g, i)) ? 1.f : 0.f;
-            Terms<T> seen;
-            seen.set(ones);
-#pragma unroll
-            for (int c = 0; c < L::CT; ++c)
-#pragma unroll
-              for (int which = 1; which <= 2; ++which) {
-                uint32_t x[L::VW];
-#pragma unroll
-                for (int e = 0; e < L::VW; ++e) x[e] = only<F>(vr[c][e], which);
-                const f32x4 n = value_tile<F>(x, seen, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (n[e] > 0.f) o[r][c][e] += which == 1 ? kInf : -kInf;
-              }
-          }
-#pragma unroll
-          for (int c = 0; c < L::CT; ++c)
-#pragma unroll
-            for (int e = 0; e < L::VW; ++e) vr[c][e] = only<F>(vr[c][e], 0);
-        }
-      }
+      // What a row does not see must not reach it, but 0 times a NaN or an
+      // infinity is NaN: those are taken out of the operand, and added below
+      // to the rows that see them.
+      bad = clear_tail<F, DH>(vr, g, wh.ctx - kb);
     }
 #pragma unroll
     for (int c = 0; c < L::CT; ++c)
 #pragma unroll
       for (int r = 0; r < R; ++r) o[r][c] = value_tile<F>(vr[c], terms[r], o[r][c]);
+    if constexpr (F != EVO_CACHE_INT8) {
+      if (__builtin_expect(__any(bad), 0)) {
+        int slot;
+        const int64_t b = block_base(kb, &slot);
+#pragma unroll 1
+        for (int j = 0; j < min(kKeys, wh.ctx - kb); ++j) {
+          int64_t at = ((b * DH + 4 * g) << ps) + slot + j;
+          asm volatile("" : "+v"(at));  // the addresses are made here, not kept over the loop
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const bool see = sees(a, wh, pos[r], kb + j);
+#pragma unroll
+            for (int c = 0; c < L::CT; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float x = not_finite<F>(a.cache.v, at + ((c * 16 + e) << ps));
+                if (see) o[r][c][e] += x;
+                __builtin_amdgcn_sched_barrier(0);
+              }
+          }
+        }
+      }
+    }
     __builtin_amdgcn_sched_barrier(0);
     if (next >= 0) load_values(next);
     __builtin_amdgcn_sched_barrier(0);
@@ -718,7 +712,7 @@ template <int F, int DH, int NW> struct Stage {
           bool found = false;
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
-            const uint32_t y = only<F>(x[d], 0);
+            const uint32_t y = finite_only<F>(x[d]);
             found |= y != x[d];
             x[d] = y;
           }
@@ -952,19 +946,14 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
 #pragma unroll 1
           for (int j = 0; j < min(kKeys, wh.ctx - kb); ++j) {
             const bool see = sees(a, wh, pos, kb + j);
+            int64_t at = ((b * DH + 4 * half) << ps) + s0 + j;
+            asm volatile("" : "+v"(at));  // 64 addresses are made here, not kept over the loop
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
-                const int64_t at = ((b * DH + c * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) << ps) + s0 + j;
-                uint32_t x;
-                if constexpr (F == EVO_CACHE_FP8) {
-                  x = reinterpret_cast<const uint8_t*>(a.cache.v)[at];
-                  x = (x & 0x7f) == 0x7f ? 0x7fc00000u : 0;
-                } else {
-                  x = (uint32_t)reinterpret_cast<const uint16_t*>(a.cache.v)[at] << 16;
-                }
-                if (see && (x & 0x7f800000u) == 0x7f800000u) o[c][e] += __builtin_bit_cast(float, x);
+                const float x = not_finite<F>(a.cache.v, at + ((c * 32 + 8 * (e >> 2) + (e & 3)) << ps));
+                if (see) o[c][e] += x;
                 __builtin_amdgcn_sched_barrier(0);
               }
           }
@@ -1003,35 +992,52 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
     a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Joins the parts of a row tile, in order.
+// Joins the parts of a row tile, in order, a thread four channels of a row;
+// eight parts are requested at a time, since a part's load is all latency.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
-  const int th = blockIdx.x, h = th % a.cache.n_kv_heads, tile = th / a.cache.n_kv_heads;
+  constexpr int AT = 8;
+  const int x = (blockIdx.x * 256 + threadIdx.x) % (tile_rows * (DH / 4));
+  const int th = (blockIdx.x * 256 + threadIdx.x) / (tile_rows * (DH / 4));
+  const int h = th % a.cache.n_kv_heads, tile = th / a.cache.n_kv_heads;
   int seq;
   Where wh;
-  if (!find_tile(a, tile, tile_rows, &seq, &wh)) return;
-  for (int x = threadIdx.x; x < tile_rows * (DH / 4); x += 256) {
-    const int r = x / (DH / 4), c = x % (DH / 4) * 4, row = wh.base + r;
-    if (row >= wh.rows) break;
-    const int64_t part = (int64_t)th * a.n_split * tile_rows + r;
-    float M = -kInf;
-    for (int s = 0; s < a.n_split; ++s) M = fmaxf(M, a.part_ml[(part + (int64_t)s * tile_rows) * 2]);
-    const float base = M == -kInf ? 0.f : M;
-    float t = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.n_split; ++s) {
-      const int64_t at = part + (int64_t)s * tile_rows;
-      const float l = a.part_ml[at * 2 + 1], f = exp2_(a.part_ml[at * 2] - base);
-      if (l == 0.f) continue;  // (a part that saw nothing wrote no outputs)
-      t += l * f;
-      o += *reinterpret_cast<const f32x4*>(a.part + at * DH + c) * f;
+  if (tile >= a.n_tiles || !find_tile(a, tile, tile_rows, &seq, &wh)) return;
+  const int r = x / (DH / 4), c = x % (DH / 4) * 4, row = wh.base + r;
+  if (row >= wh.rows) return;
+  const int64_t part = (int64_t)th * a.n_split * tile_rows + r;
+  float M = -kInf, t = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < a.n_split; s0 += AT) {
+    float m[AT], l[AT];
+    f32x4 v[AT];
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const int64_t at = part + (int64_t)min(s0 + i, a.n_split - 1) * tile_rows;
+      m[i] = a.part_ml[at * 2];
+      l[i] = s0 + i < a.n_split ? a.part_ml[at * 2 + 1] : 0.f;
+      v[i] = *reinterpret_cast<const f32x4*>(a.part + at * DH + c);
     }
-    const int tok = row / a.group, head = h * a.group + row - tok * a.group;
-    T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
-    store4(dst + c, a.wide, t == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / t));
-    if (a.lse && c == 0)
-      a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = t == 0.f ? -kInf : (M + __builtin_amdgcn_logf(t)) * kLn2;
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < AT; ++i) top = fmaxf(top, m[i]);
+    const float base = top == -kInf ? 0.f : top, keep = exp2_(M - base);
+    M = top;
+    t *= keep;
+    o *= keep;
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const float f = exp2_(m[i] - base);
+      if (l[i] == 0.f) continue;  // (a part that saw nothing wrote no outputs)
+      t += l[i] * f;
+      o += v[i] * f;
+    }
   }
+  const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+  T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
+  store4(dst + c, a.wide, t == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / t));
+  if (a.lse && c == 0)
+    a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = t == 0.f ? -kInf : (M + __builtin_amdgcn_logf(t)) * kLn2;
 }
 
 template <typename T, int F, int DH>
@@ -1050,7 +1056,8 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((stream_kernel<T, F, DH, 2>), dim3(blocks * p.n_split), dim3(kWaves * 64), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_split == 1) return e;
-  hipLaunchKernelGGL((join_kernel<T, DH>), dim3(blocks), dim3(256), 0, stream, a, p.tile_rows);
+  hipLaunchKernelGGL((join_kernel<T, DH>), dim3((blocks * p.tile_rows * (DH / 4) + 255) / 256), dim3(256), 0, stream, a,
+                     p.tile_rows);
   return hipGetLastError();
 }
 

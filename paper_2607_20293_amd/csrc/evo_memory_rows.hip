@@ -30,6 +30,7 @@ constexpr int kNone = -1;
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;     // heads whose rows a lane requests ahead
 constexpr int kFill = 2048;   // workgroups that fill the device (8 a compute unit)
+constexpr int kValueWaves = 1024;
 
 template <int F> struct Held;
 template <> struct Held<EVO_CACHE_FP32> { typedef float type; };
@@ -147,18 +148,41 @@ __device__ __forceinline__ int64_t block_of(const RowsArgs& a, int seq, int pos,
   return (int64_t)page_of(a.rows, a.cache, seq, pos >> a.cache.page_shift) * a.cache.n_kv_heads + head;
 }
 
-// 8 consecutive keys of a cache row
-template <int F> __device__ __forceinline__ void store_key(const RowsArgs& a, int64_t at, int lane, const float* y,
-                                                            const Coding& c) {
+// (selected as numbers: a choice between two members of the arguments would put
+// them into memory)
+__device__ __forceinline__ float* scales_of(const RowsArgs& a, bool value) {
+  const uint64_t k = (uint64_t)a.cache.ks, v = (uint64_t)a.cache.vs;
+  return reinterpret_cast<float*>(value ? v : k);
+}
+
+// The lane's 8 values of a row into the cache: keys side by side, values a page
+// row each.
+template <int F, int DH>
+__device__ __forceinline__ void store_held(const RowsArgs& a, int64_t block, int slot, bool value, int lane, const float* y,
+                                           const Coding& c) {
   typedef typename Held<F>::type H;
-  H* p = reinterpret_cast<H*>(a.cache.k) + at + lane * 8;
+  const int ps = a.cache.page_shift;
+  H* k = reinterpret_cast<H*>(a.cache.k) + ((block << ps) + slot) * DH + lane * 8;
+  H* v = reinterpret_cast<H*>(a.cache.v) + ((block * DH + lane * 8) << ps) + slot;
   if constexpr (is_coded(F)) {
     float z[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] = quotient<F>(y[e], c);
-    *reinterpret_cast<u32x2*>(p) = u32x2{code4<F>(z), code4<F>(z + 4)};
+    const u32x2 w = {code4<F>(z), code4<F>(z + 4)};
+    if (!value) {
+      *reinterpret_cast<u32x2*>(k) = w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[(int64_t)e << ps] = (H)(w[e / 4] >> (8 * (e & 3)));
+    }
+    if (lane == 0) scales_of(a, value)[(block << ps) + slot] = c.s;
   } else if constexpr (F != kNone) {
-    store8(p, 1, y);
+    if (!value) {
+      store8(k, 1, y);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[(int64_t)e << ps] = (H)y[e];
+    }
   }
 }
 
@@ -188,7 +212,7 @@ __device__ __forceinline__ void unpack(const Raw<float>& r, float* x) {
 template <typename T, int F, int DH>
 __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
   constexpr int LPR = DH / 8;  // lanes a row
-  const int heads = a.n_heads + a.n_kv_heads, groups = a.head_groups;
+  const int heads = a.heads_by_rows, groups = a.head_groups;
   const int lane = threadIdx.x % LPR;
   const int tok = (block / groups) * (kThreads / LPR) + (int)threadIdx.x / LPR, h0 = block % groups;
   // whole waves stay for the exchanges; rows past the end repeat the last one
@@ -196,8 +220,11 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
   const bool live = tok < a.rows.n_rows;
   const int n = live ? tok : a.rows.n_rows - 1;
   const auto source = [&](int h) {
-    return (h < a.n_heads ? reinterpret_cast<const T*>(a.q.p) + n * a.q.row + h * a.q.head
-                          : reinterpret_cast<const T*>(a.k.p) + n * a.k.row + (h - a.n_heads) * a.k.head) + lane * 8;
+    const int hk = h - a.n_heads, hv = hk - a.n_kv_heads;
+    const T* p = hk < 0 ? reinterpret_cast<const T*>(a.q.p) + n * a.q.row + h * a.q.head
+                 : hv < 0 ? reinterpret_cast<const T*>(a.k.p) + n * a.k.row + hk * a.k.head
+                          : reinterpret_cast<const T*>(a.v.p) + n * a.v.row + hv * a.v.head;
+    return p + lane * 8;
   };
   Raw<T> next[kAhead];
 #pragma unroll
@@ -250,11 +277,11 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
   const int partner = (threadIdx.x & 63) + (lane < half_lanes ? half_lanes : lane < 2 * half_lanes ? -half_lanes : 0);
 
   const auto one = [&](int h, const Raw<T>& raw) {
-    const bool is_q = h < a.n_heads;
-    const int hk = h - a.n_heads;
+    const bool is_q = h < a.n_heads, is_v = F != kNone && h >= a.n_heads + a.n_kv_heads;
+    const int hk = h - a.n_heads - (is_v ? a.n_kv_heads : 0);
     float x[8];
     unpack(raw, x);
-    if (a.norm) {
+    if (a.norm && !is_v) {
       float ss = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
@@ -264,7 +291,7 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = x[e] * r * (is_q ? qg[e] : kg[e]);
     }
-    if (a.half) {
+    if (a.half && !is_v) {
       float o[8];
       if (a.adjacent) {
 #pragma unroll
@@ -294,11 +321,7 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
       c = coding_of<F>(top);
     }
     const int64_t b = block_of(a, seq, pos, hk);
-    if (live && b >= 0) {
-      const int64_t row = (b << a.cache.page_shift) + (pos & ((1 << a.cache.page_shift) - 1));
-      store_key<F>(a, row * DH, lane, x, c);
-      if (is_coded(F) && lane == 0) a.cache.ks[row] = c.s;
-    }
+    if (live && b >= 0) store_held<F, DH>(a, b, pos & ((1 << a.cache.page_shift) - 1), is_v, lane, x, c);
   };
   for (int h = h0; h < heads; h += kAhead * groups) {
     Raw<T> now[kAhead];
@@ -460,23 +483,37 @@ __device__ __forceinline__ void read_keys(const RowsArgs& a, int block) {
   find_row(a.rows, n, &seq, &i);
   const int pos = a.starts[seq] + i;
   const int64_t b = block_of(a, seq, pos, 0);
-  for (int h = block % groups; h < a.n_kv_heads; h += groups) {
+  for (int h = block % groups; h < a.heads_by_rows; h += groups) {
+    const bool is_v = h >= a.n_kv_heads;
+    const int hk = is_v ? h - a.n_kv_heads : h;
     float x[8] = {};
     if (b >= 0) {
-      const int64_t row = ((b + h) << ps) + (pos & ((1 << ps) - 1));
-      const H* p = reinterpret_cast<const H*>(a.cache.k) + row * DH + lane * 8;
+      const int64_t row = ((b + hk) << ps) + (pos & ((1 << ps) - 1));
+      const H* k = reinterpret_cast<const H*>(a.cache.k) + row * DH + lane * 8;
+      const H* v = reinterpret_cast<const H*>(a.cache.v) + (((b + hk) * DH + lane * 8) << ps) + (pos & ((1 << ps) - 1));
       if constexpr (is_coded(F)) {
-        const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-        const float s = a.cache.ks[row];
-        decode4<F>(v[0], x);
-        decode4<F>(v[1], x + 4);
+        u32x2 w = {0, 0};
+        if (!is_v) {
+          w = *reinterpret_cast<const u32x2*>(k);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(uint8_t)v[(int64_t)e << ps] << (8 * (e & 3));
+        }
+        const float s = scales_of(a, is_v)[row];
+        decode4<F>(w[0], x);
+        decode4<F>(w[1], x + 4);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] *= s;
+      } else if (!is_v) {
+        load8(k, 1, x);
       } else {
-        load8(p, 1, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)v[(int64_t)e << ps];
       }
     }
-    store8(reinterpret_cast<T*>(a.ko.p) + n * a.ko.row + h * a.ko.head + lane * 8, a.wide, x);
+    T* dst = is_v ? reinterpret_cast<T*>(a.v.p) + n * a.v.row + hk * a.v.head
+                  : reinterpret_cast<T*>(a.ko.p) + n * a.ko.row + hk * a.ko.head;
+    store8(dst + lane * 8, a.wide, x);
   }
 }
 
@@ -539,32 +576,32 @@ __global__ void __launch_bounds__(kThreads) read_kernel(RowsArgs a) {
   else read_values<T, F, DH>(a, blockIdx.x - a.qk_blocks, stage[threadIdx.x >> 6]);
 }
 
-int v_blocks(const RowsArgs& a) {
-  const int64_t waves = ((int64_t)a.rows.n_rows + 63) / 64 * a.n_kv_heads;
-  return (int)((waves + kThreads / 64 - 1) / (kThreads / 64));
-}
-
-// Workgroups of the part that takes a token's heads in turn: as few groups of
-// heads as still fill the device.
-template <int DH> void spread_heads(RowsArgs* a, int heads) {
+// How a launch is divided.  Values go the way of keys, a group of lanes a row,
+// where the waves of 64 rows of their own would not fill the device.
+// Else the part that takes a token's heads in turn: as few groups of heads as
+// still fill the device.
+template <int DH> int divide(RowsArgs* a, bool values) {
   constexpr int per = kThreads / (DH / 8);  // tokens of a workgroup
+  const int64_t waves = values ? ((int64_t)a->rows.n_rows + 63) / 64 * a->n_kv_heads : 0;
+  const bool by_rows = values && waves < kValueWaves;
+  a->heads_by_rows = a->n_heads + a->n_kv_heads + (by_rows ? a->n_kv_heads : 0);
   const int64_t blocks = ((int64_t)a->rows.n_rows + per - 1) / per;
-  a->head_groups = (int)std::max<int64_t>(1, std::min<int64_t>(heads, (kFill + blocks - 1) / blocks));
+  a->head_groups = (int)std::max<int64_t>(1, std::min<int64_t>(a->heads_by_rows, (kFill + blocks - 1) / blocks));
   a->qk_blocks = (int)(blocks * a->head_groups);
+  return a->qk_blocks + (by_rows ? 0 : (int)((waves + kThreads / 64 - 1) / (kThreads / 64)));
 }
 
 template <typename T, int F, int DH>
 hipError_t launch_rows_as(RowsArgs a, hipStream_t stream) {
-  spread_heads<DH>(&a, a.n_heads + a.n_kv_heads);
-  hipLaunchKernelGGL((rows_kernel<T, F, DH>), dim3(a.qk_blocks + (F == kNone ? 0 : v_blocks(a))), dim3(kThreads), 0,
-                     stream, a);
+  const int blocks = divide<DH>(&a, F != kNone);
+  hipLaunchKernelGGL((rows_kernel<T, F, DH>), dim3(blocks), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
 template <typename T, int F, int DH>
 hipError_t launch_read_as(RowsArgs a, hipStream_t stream) {
-  spread_heads<DH>(&a, a.n_kv_heads);
-  hipLaunchKernelGGL((read_kernel<T, F, DH>), dim3(a.qk_blocks + v_blocks(a)), dim3(kThreads), 0, stream, a);
+  const int blocks = divide<DH>(&a, true);
+  hipLaunchKernelGGL((read_kernel<T, F, DH>), dim3(blocks), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

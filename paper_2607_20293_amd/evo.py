@@ -12,6 +12,7 @@ import sys
 from typing import Optional, Sequence
 
 import numpy as np
+import torch
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libevo.so")
 
@@ -643,7 +644,6 @@ _ref = ctypes.byref
 
 
 def _row_dtype(t) -> int:
-    import torch
     if t.dtype == torch.bfloat16:
         return EVO_BF16
     if t.dtype == torch.float32:
@@ -651,83 +651,71 @@ def _row_dtype(t) -> int:
     raise TypeError(f"expected float32 or bfloat16 rows, got {t.dtype}")
 
 
-def _heads(name, t, dtype, rows, heads, dh, device) -> Heads:
-    """A [rows][heads][dh] tensor with any row and head strides."""
+# The checks below run at every call of operators that take a few microseconds:
+# one comparison of everything, the reason looked for only where it fails.
+def _wrong(name, t, dtype, shape, device):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a tensor")
     if t.dtype != dtype or t.device != device:
         raise TypeError(f"{name}: expected {dtype} on {device}, got {t.dtype} on {t.device}")
-    if t.shape != (rows, heads, dh):
-        raise ValueError(f"{name}: expected shape {(rows, heads, dh)}, got {tuple(t.shape)}")
-    s = t.stride()
-    if s[2] != 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
-    return Heads(t.data_ptr(), s[0], s[1])
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{name}: must be contiguous (of rows [rows][heads][dh]: the last dimension)")
 
 
-def _ints(name, t, shape, device) -> int:
-    import torch
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.device != device:
-        raise TypeError(f"{name}: expected an int32 tensor on {device}")
-    if t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t.data_ptr()
+def _heads(name, t, dtype, shape, device) -> Heads:
+    """A [rows][heads][dh] tensor with any row and head strides."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape:
+        _wrong(name, t, dtype, shape, device)
+    row, head, one = t.stride()
+    if one != 1:
+        _wrong(name, t, dtype, shape, device)
+    return Heads(t.data_ptr(), row, head)
 
 
-def _floats(name, t, shape, device):
-    import torch
-    if t is None:
-        return None
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.device != device:
-        raise TypeError(f"{name}: expected a float32 tensor on {device}")
-    if t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+def _ptr(name, t, dtype, shape, device) -> int:
+    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
+            or not t.is_contiguous()):
+        _wrong(name, t, dtype, shape, device)
     return t.data_ptr()
 
 
 def _device_of(t):
-    import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("expected a HIP device tensor")
     return t.device
 
 
-class _On:
-    """The stream of a call: the caller's, or the device's current one.  Makes
-    the device current; tensors allocated here for a stream that is not the
-    current one are kept until its work is done."""
+def _current_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
 
-    def __init__(self, device, stream):
-        import torch
-        self.device, self.given = device, stream
-        self.current = torch.cuda.current_stream(device)
-        self.stream = self.current if stream is None else stream
-        self.other = None
-        if torch.cuda.current_device() != device.index:
-            self.other = torch.cuda.device(device)
-            self.other.__enter__()
 
-    def __enter__(self):
-        return self
+# (the handle alone, without the Stream object around it, where torch has that)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
 
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
 
-    @property
-    def handle(self):
-        return self.stream.cuda_stream
-
-    def empty(self, shape, dtype):
-        import torch
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self.given is not None and self.given != self.current:
-            t.record_stream(self.given)
-        return t
+def _enqueue(device, stream, made, call, *args):
+    """call(*args, stream handle) with the device current.  Tensors made here
+    for a stream that is not the current one are kept until its work is done."""
+    if stream is None:
+        handle = _current_stream(device.index)
+    else:
+        handle = stream.cuda_stream
+        if handle != _current_stream(device.index):
+            for t in made:
+                t.record_stream(stream)
+    if torch.cuda.current_device() == device.index:
+        rc = call(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, handle)
+    if rc != 0:
+        _check(rc)
 
 
 def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, device="cuda"):
     """(cos, sin) of position * theta^(-2i / rotary_dim), float32
     [n_positions][rotary_dim / 2][2], computed in 64 bits."""
-    import torch
     inv = theta ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64, device=device) / rotary_dim)
     a = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * inv
     return torch.stack([a.cos(), a.sin()], dim=-1).float().contiguous()
@@ -741,29 +729,27 @@ class KVCache:
     k_scale and v_scale, float32 [pages][heads][page_size]."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        import torch
         device = _device_of(k)
         formats = {torch.float32: CACHE_FP32, torch.bfloat16: CACHE_BF16, torch.int8: CACHE_INT8,
                    torch.float8_e4m3fn: CACHE_FP8}
         if k.dtype not in formats:
             raise TypeError(f"no cache format holds {k.dtype}")
-        if k.dim() != 4 or v.dtype != k.dtype or v.device != device:
-            raise ValueError("k must be [pages][heads][page_size][dh], v of its type on its device")
+        if k.dim() != 4:
+            raise ValueError("k must be [pages][heads][page_size][dh]")
         pages, heads, size, dh = k.shape
-        if v.shape != (pages, heads, dh, size) or not k.is_contiguous() or not v.is_contiguous():
-            raise ValueError("v must be [pages][heads][dh][page_size], and both contiguous")
+        kp, vp = _ptr("k", k, k.dtype, k.shape, device), _ptr("v", v, k.dtype, (pages, heads, dh, size), device)
         fmt = formats[k.dtype]
         if (fmt >= CACHE_INT8) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
             raise ValueError("8-bit caches have scales, the others have none")
-        ks, vs = (_floats(n, t, (pages, heads, size), device) for n, t in (("k_scale", k_scale), ("v_scale", v_scale)))
+        ks, vs = (None if t is None else _ptr(n, t, torch.float32, (pages, heads, size), device)
+                  for n, t in (("k_scale", k_scale), ("v_scale", v_scale)))
         self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, device
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pages, heads, size, dh
-        self.desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), ks, vs, fmt, pages, size, heads, dh)
+        self.desc = KVCacheDesc(kp, vp, ks, vs, fmt, pages, size, heads, dh)
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 64, dtype=None, device="cuda"):
         """An unwritten cache of its own tensors (dtype: bfloat16 by default)."""
-        import torch
         dtype = torch.bfloat16 if dtype is None else dtype
         k = torch.empty((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
         v = torch.empty((n_pages, n_kv_heads, head_dim, page_size), dtype=dtype, device=device)
@@ -774,32 +760,36 @@ class KVCache:
     def rows(self, page_table, n_rows: int, cu_rows, max_rows) -> KVRows:
         """The rows of a call (evo_kv_rows): page_table int32 [seqs][pages];
         cu_rows int32 [seqs + 1] or None (as many rows in every sequence)."""
-        if page_table.dim() != 2:
+        shape = page_table.shape
+        if len(shape) != 2:
             raise ValueError("page_table must be [sequences][pages]")
-        seqs, wide = page_table.shape
-        if cu_rows is None:
-            if seqs == 0 or n_rows % seqs:
-                raise ValueError(f"{n_rows} rows over {seqs} sequences need cu_rows")
+        seqs, wide = shape
+        cu = None
+        if cu_rows is not None:
+            cu = _ptr("cu_rows", cu_rows, torch.int32, (seqs + 1,), self.device)
+            if max_rows is None:
+                max_rows = n_rows
+        elif seqs == 0 or n_rows % seqs:
+            raise ValueError(f"{n_rows} rows over {seqs} sequences need cu_rows")
+        else:
             max_rows = n_rows // seqs
-        elif max_rows is None:
-            max_rows = n_rows
-        return KVRows(seqs, n_rows, max_rows, wide,
-                      None if cu_rows is None else _ints("cu_rows", cu_rows, (seqs + 1,), self.device),
-                      _ints("page_table", page_table, (seqs, wide), self.device))
+        return KVRows(seqs, n_rows, max_rows, wide, cu, _ptr("page_table", page_table, torch.int32, shape, self.device))
 
 
 def _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device) -> NormRope:
     if pairs not in _PAIRS:
         raise ValueError("pairs must be 'halves' or 'adjacent'")
     rotary = n_positions = 0
+    tp = None
     if table is not None:
         if table.dim() != 3:
             raise ValueError("table must be [positions][rotary_dim / 2][2]")
-        n_positions, rotary = table.shape[0], 2 * table.shape[1]
-        _floats("table", table, (n_positions, rotary // 2, 2), device)
+        n_positions, half, _ = table.shape
+        rotary = 2 * half
+        tp = _ptr("table", table, torch.float32, (n_positions, half, 2), device)
     return NormRope(rotary, _PAIRS[pairs], n_positions, -1.0 if eps is None else eps,
-                    _floats("q_gain", q_gain, (dh,), device), _floats("k_gain", k_gain, (dh,), device),
-                    None if table is None else table.data_ptr())
+                    None if q_gain is None else _ptr("q_gain", q_gain, torch.float32, (dh,), device),
+                    None if k_gain is None else _ptr("k_gain", k_gain, torch.float32, (dh,), device), tp)
 
 
 def qk_norm_rope(q, k, positions, table, q_gain=None, k_gain=None, eps: Optional[float] = 1e-6, pairs: str = "halves",
@@ -810,48 +800,46 @@ def qk_norm_rope(q, k, positions, table, q_gain=None, k_gain=None, eps: Optional
     (float32 [n_positions][rotary_dim / 2][2]; None: not).  out: (q_out,
     k_out), which may be (q, k).  Returns (q_out, k_out)."""
     device = _device_of(q)
-    dt = _row_dtype(q)
+    dt, dtype = _row_dtype(q), q.dtype
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [rows][heads][dh]")
-    n, hq, dh = q.shape
+    qs = q.shape
+    n, hq, dh = qs
     hk = k.shape[1]
+    ks = (n, hk, dh)
     nr = _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device)
-    with _On(device, stream) as on:
-        q_out, k_out = (on.empty((n, hq, dh), q.dtype), on.empty((n, hk, dh), q.dtype)) if out is None else out
-        _check(lib().evo_qk_norm_rope(
-            _ref(nr), dt, dh, n, hq, hk, _ref(_heads("q", q, q.dtype, n, hq, dh, device)),
-            _ref(_heads("k", k, q.dtype, n, hk, dh, device)),
-            None if table is None else _ints("positions", positions, (n,), device),
-            _ref(_heads("q_out", q_out, q.dtype, n, hq, dh, device)),
-            _ref(_heads("k_out", k_out, q.dtype, n, hk, dh, device)), on.handle))
+    made = (q.new_empty(qs), q.new_empty(ks)) if out is None else ()
+    q_out, k_out = made or out
+    _enqueue(device, stream, made, lib().evo_qk_norm_rope, _ref(nr), dt, dh, n, hq, hk,
+             _ref(_heads("q", q, dtype, qs, device)), _ref(_heads("k", k, dtype, ks, device)),
+             None if table is None else _ptr("positions", positions, torch.int32, (n,), device),
+             _ref(_heads("q_out", q_out, dtype, qs, device)), _ref(_heads("k_out", k_out, dtype, ks, device)))
     return q_out, k_out
 
 
 def cache_write(cache: KVCache, page_table, starts, k, v, cu_rows=None, max_rows: Optional[int] = None, stream=None):
     """evo_cache_write: k, v [rows][kv_heads][dh] into the cache, row i of
     sequence s at position starts[s] + i (int32 [sequences])."""
-    n, dh, device = k.shape[0], cache.head_dim, cache.device
-    dt = _row_dtype(k)
-    rows = cache.rows(page_table, n, cu_rows, max_rows)
-    with _On(device, stream) as on:
-        _check(lib().evo_cache_write(
-            _ref(cache.desc), _ref(rows), dt, _ints("starts", starts, (rows.n_seqs,), device),
-            _ref(_heads("k", k, k.dtype, n, cache.n_kv_heads, dh, device)),
-            _ref(_heads("v", v, k.dtype, n, cache.n_kv_heads, dh, device)), on.handle))
+    device, dtype = cache.device, k.dtype
+    dt, shape = _row_dtype(k), (k.shape[0], cache.n_kv_heads, cache.head_dim)
+    rows = cache.rows(page_table, shape[0], cu_rows, max_rows)
+    _enqueue(device, stream, (), lib().evo_cache_write, _ref(cache.desc), _ref(rows), dt,
+             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), _ref(_heads("k", k, dtype, shape, device)),
+             _ref(_heads("v", v, dtype, shape, device)))
 
 
 def cache_read(cache: KVCache, page_table, starts, n_rows: int, dtype, cu_rows=None, max_rows: Optional[int] = None,
                out=None, stream=None):
     """evo_cache_read: positions starts[s] + i of every sequence as (k, v),
     [n_rows][kv_heads][dh] of dtype."""
-    dh, device = cache.head_dim, cache.device
+    device, shape = cache.device, (n_rows, cache.n_kv_heads, cache.head_dim)
     rows = cache.rows(page_table, n_rows, cu_rows, max_rows)
-    with _On(device, stream) as on:
-        shape = (n_rows, cache.n_kv_heads, dh)
-        k, v = (on.empty(shape, dtype), on.empty(shape, dtype)) if out is None else out
-        _check(lib().evo_cache_read(
-            _ref(cache.desc), _ref(rows), _row_dtype(k), _ints("starts", starts, (rows.n_seqs,), device),
-            _ref(_heads("k_out", k, dtype, *shape, device)), _ref(_heads("v_out", v, dtype, *shape, device)), on.handle))
+    new = cache.k.new_empty
+    made = (new(shape, dtype=dtype), new(shape, dtype=dtype)) if out is None else ()
+    k, v = made or out
+    _enqueue(device, stream, made, lib().evo_cache_read, _ref(cache.desc), _ref(rows), _row_dtype(k),
+             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device),
+             _ref(_heads("k_out", k, dtype, shape, device)), _ref(_heads("v_out", v, dtype, shape, device)))
     return k, v
 
 
@@ -861,21 +849,20 @@ def qkv_write(cache: KVCache, page_table, starts, q, k, v, table, q_gain=None, k
     """evo_qkv_write: q normalised and rotated into q_out (returned), k
     normalised, rotated and written, v written; rotation by the positions
     starts[s] + i that are written."""
-    device, dh = cache.device, cache.head_dim
+    device, dh, dtype = cache.device, cache.head_dim, q.dtype
     dt = _row_dtype(q)
     if q.dim() != 3:
         raise ValueError("q must be [rows][heads][dh]")
     n, hq = q.shape[0], q.shape[1]
+    qs, ks = (n, hq, dh), (n, cache.n_kv_heads, dh)
     rows = cache.rows(page_table, n, cu_rows, max_rows)
     nr = _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device)
-    with _On(device, stream) as on:
-        q_out = on.empty((n, hq, dh), q.dtype) if q_out is None else q_out
-        _check(lib().evo_qkv_write(
-            _ref(cache.desc), _ref(rows), _ref(nr), dt, hq, _ints("starts", starts, (rows.n_seqs,), device),
-            _ref(_heads("q", q, q.dtype, n, hq, dh, device)),
-            _ref(_heads("k", k, q.dtype, n, cache.n_kv_heads, dh, device)),
-            _ref(_heads("v", v, q.dtype, n, cache.n_kv_heads, dh, device)),
-            _ref(_heads("q_out", q_out, q.dtype, n, hq, dh, device)), on.handle))
+    made = (q.new_empty(qs),) if q_out is None else ()
+    q_out, = made or (q_out,)
+    _enqueue(device, stream, made, lib().evo_qkv_write, _ref(cache.desc), _ref(rows), _ref(nr), dt, hq,
+             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), _ref(_heads("q", q, dtype, qs, device)),
+             _ref(_heads("k", k, dtype, ks, device)), _ref(_heads("v", v, dtype, ks, device)),
+             _ref(_heads("q_out", q_out, dtype, qs, device)))
     return q_out
 
 
@@ -888,29 +875,40 @@ def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_ro
     slopes: float32 [heads] or None; max_length: a bound of lengths, for the
     plan alone (0: the page table's).  Returns (out [rows][heads][dh], lse
     float32 [rows][heads])."""
-    import torch
-    device, dh = cache.device, cache.head_dim
+    device, dh, dtype = cache.device, cache.head_dim, q.dtype
+    if torch.cuda.current_device() != device.index:  # (the plan is the current device's)
+        with torch.cuda.device(device):
+            return chunk_attention(q, cache, page_table, lengths, cu_rows, max_rows, scale=scale, causal=causal,
+                                   window=window, cap=cap, slopes=slopes, prefix=prefix, starts=starts,
+                                   max_length=max_length, out=out, lse=lse, stream=stream)
     dt = _row_dtype(q)
     if q.dim() != 3:
         raise ValueError("q must be [rows][heads][dh]")
     n, hq = q.shape[0], q.shape[1]
+    qs = (n, hq, dh)
     rows = cache.rows(page_table, n, cu_rows, max_rows)
-    seqs = (rows.n_seqs,)
+    seqs, i32 = (rows.n_seqs,), torch.int32
     att = Attention(dt, hq, 1 if causal else 0, window, max_length, dh ** -0.5 if scale is None else scale, cap,
-                    _ints("lengths", lengths, seqs, device),
-                    None if starts is None else _ints("starts", starts, seqs, device),
-                    None if prefix is None else _ints("prefix", prefix, seqs, device),
-                    _floats("slopes", slopes, (hq,), device))
-    L = lib()
-    with _On(device, stream) as on:
-        out = on.empty((n, hq, dh), q.dtype) if out is None else out
-        lse = on.empty((n, hq), torch.float32) if lse is None else lse
-        need = L.evo_chunk_attention_workspace(_ref(cache.desc), _ref(rows), _ref(att))
+                    _ptr("lengths", lengths, i32, seqs, device),
+                    None if starts is None else _ptr("starts", starts, i32, seqs, device),
+                    None if prefix is None else _ptr("prefix", prefix, i32, seqs, device),
+                    None if slopes is None else _ptr("slopes", slopes, torch.float32, (hq,), device))
+    L, desc = lib(), cache.desc
+    made = []
+    if out is None:
+        out = q.new_empty(qs)
+        made.append(out)
+    if lse is None:
+        lse = q.new_empty((n, hq), dtype=torch.float32)
+        made.append(lse)
+    hs, ho = _heads("q", q, dtype, qs, device), _heads("out", out, dtype, qs, device)
+    need = L.evo_chunk_attention_workspace(_ref(desc), _ref(rows), _ref(att))
+    work = None
+    if need:
         if need < 0:
             _check(int(need))
-        work = on.empty((need,), torch.uint8) if need else None
-        _check(L.evo_chunk_attention(
-            _ref(cache.desc), _ref(rows), _ref(att), _ref(_heads("q", q, q.dtype, n, hq, dh, device)),
-            _ref(_heads("out", out, q.dtype, n, hq, dh, device)), _floats("lse", lse, (n, hq), device),
-            None if work is None else work.data_ptr(), need, on.handle))
+        made.append(q.new_empty((need,), dtype=torch.uint8))
+        work = made[-1].data_ptr()
+    _enqueue(device, stream, made, L.evo_chunk_attention, _ref(desc), _ref(rows), _ref(att), _ref(hs), _ref(ho),
+             _ptr("lse", lse, torch.float32, (n, hq), device), work, need)
     return out, lse
