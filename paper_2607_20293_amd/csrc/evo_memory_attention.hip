@@ -151,6 +151,17 @@ __device__ __forceinline__ Blocks blocks_of(const AttArgs& a, const Where& w) {
   return b;
 }
 
+// The pages of 64 of the blocks v, v + step, .. that a wave comes to: a lane
+// holds one, so that no block's load waits for its page's number first.
+struct Pages {
+  int held;
+  __device__ __forceinline__ void load(const AttArgs& a, const Blocks& bl, int seq, int v, int step) {
+    const int at = min(v + (int)(threadIdx.x & 63) * step, max(bl.count - 1, 0));
+    held = bl.count ? page_of(a.rows, a.cache, seq, (bl.at(at) * kKeys) >> a.cache.page_shift) : 0;
+  }
+  __device__ __forceinline__ int at(int i) const { return __builtin_amdgcn_readlane(held, i & 63); }
+};
+
 __device__ __forceinline__ bool sees(const AttArgs& a, const Where& w, int p, int j) {
   const bool near = (!a.causal || j <= p) && (!a.window || abs(p - j) < a.window);
   return j < w.ctx && (j < w.prefix || near);
@@ -371,6 +382,8 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
   const int per = max((bl.count + a.n_split - 1) / a.n_split, kWaves);
   const int v0 = split * per, v1 = min(v0 + per, bl.count);
   const int ps = a.cache.page_shift;
+  Pages pages;
+  pages.load(a, bl, seq, v0 + w, kWaves);
 
   Query<T, DH> q[R];
   int pos[R];
@@ -397,13 +410,9 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
   const uint32_t koff = (uint32_t)((L::key_of(0, lr >> 2, lr & 3) * DH + g * L::E) * L::SZ);
   const uint32_t voff = (uint32_t)(((lr << ps) + g * L::KG) * L::SZ);
   uint32_t kr[4][L::KW], vr[L::CT][L::VW];
-  const auto block_base = [&](int kb, int* slot) -> int64_t {
-    *slot = kb & ((1 << ps) - 1);
-    return (int64_t)page_of(a.rows, a.cache, seq, kb >> ps) * a.cache.n_kv_heads + h;
-  };
-  const auto load_keys = [&](int kb) {
-    int slot;
-    const int64_t b = block_base(kb, &slot);
+  const auto load_keys = [&](int kb, int page) {
+    const int slot = kb & ((1 << ps) - 1);
+    const int64_t b = (int64_t)page * a.cache.n_kv_heads + h;
     const char* p = reinterpret_cast<const char*>(a.cache.k) + ((b << ps) + slot) * (DH * L::SZ);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -421,9 +430,9 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
         }
       }
   };
-  const auto load_values = [&](int kb) {
-    int slot;
-    const int64_t b = block_base(kb, &slot);
+  const auto load_values = [&](int kb, int page) {
+    const int slot = kb & ((1 << ps) - 1);
+    const int64_t b = (int64_t)page * a.cache.n_kv_heads + h;
     const char* p = reinterpret_cast<const char*>(a.cache.v) + (((b * DH) << ps) + slot) * L::SZ;
 #pragma unroll
     for (int c = 0; c < L::CT; ++c)
@@ -436,17 +445,21 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
   };
 
   int v = v0 + w;
+  int page = pages.at(0);
   if (v < v1) {
-    load_keys(bl.at(v) * kKeys);
-    load_values(bl.at(v) * kKeys);
+    load_keys(bl.at(v) * kKeys, page);
+    load_values(bl.at(v) * kKeys, page);
   }
-  for (; v < v1; v += kWaves) {
+  for (int it = 1; v < v1; v += kWaves, ++it) {
     const int kb = bl.at(v) * kKeys, next = v + kWaves < v1 ? bl.at(v + kWaves) * kKeys : -1;
+    const int64_t b = (int64_t)page * a.cache.n_kv_heads + h;
+    const int slot = kb & ((1 << ps) - 1);
+    if ((it & 63) == 0) pages.load(a, bl, seq, v + kWaves, kWaves);
+    page = pages.at(it);
     const bool masked = !sees_all(a, wh, kb);
     float ks[4][4], vs[4][4];
     if constexpr (is_coded(F)) {
-      int slot;
-      const int64_t at = (block_base(kb, &slot) << ps) + slot;
+      const int64_t at = (b << ps) + slot;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const f32x4 x = *reinterpret_cast<const f32x4*>(a.cache.ks + at + L::key_of(t, g, 0));
@@ -461,7 +474,7 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
 #pragma unroll
       for (int r = 0; r < R; ++r) s[r][t] = score_tile<F, DH>(kr[t], q[r]);
     __builtin_amdgcn_sched_barrier(0);
-    if (next >= 0) load_keys(next);
+    if (next >= 0) load_keys(next, page);
     __builtin_amdgcn_sched_barrier(0);
 
     Terms<T> terms[R];
@@ -545,8 +558,6 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
       for (int r = 0; r < R; ++r) o[r][c] = value_tile<F>(vr[c], terms[r], o[r][c]);
     if constexpr (F != EVO_CACHE_INT8) {
       if (__builtin_expect(__any(bad), 0)) {
-        int slot;
-        const int64_t b = block_base(kb, &slot);
 #pragma unroll 1
         for (int j = 0; j < min(kKeys, wh.ctx - kb); ++j) {
           int64_t at = ((b * DH + 4 * g) << ps) + slot + j;
@@ -567,7 +578,7 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (next >= 0) load_values(next);
+    if (next >= 0) load_values(next, page);
     __builtin_amdgcn_sched_barrier(0);
   }
 
@@ -651,8 +662,9 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
 // products, with 32x32 matrix instructions.
 //  * LDS holds two blocks as bf16 (codes converted on the way); the next block
 //    waits in registers while this one is multiplied, one barrier a block.
-//  * 16-byte chunks of an LDS row are exchanged by the row's number (key_turn,
-//    channel & 7), so that the 8 lanes of a read's phase meet 8 bank groups.
+//  * 16-byte chunks of an LDS row are exchanged by the row's number (turn_of): a
+//    16-byte read serves lanes 0-3, 12-15 and 20-27 together, then 4-11, 16-19
+//    and 28-31 (measured), and these 16 rows meet the 16 places of 256 bytes.
 //  * The maximum moves only when a row's scores outgrow it by 2^8: terms stay
 //    below 2^8 of the true maximum's, and the outputs are seldom rescaled.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -660,7 +672,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // The LDS row of a block's key that matrix row r of a 32-key tile takes: bits 2
 // and 3 exchanged, which leaves a lane with runs of 8 keys.
 __device__ __forceinline__ int key_row(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
-__device__ __forceinline__ int key_turn(int key) { return (key & 3) | ((key >> 1) & 4); }
+// what a row of C chunks of 16 bytes exchanges its chunks by (exclusive or)
+template <int C> __device__ __forceinline__ int turn_of(int row) { return (row / (16 / C)) & (C - 1); }
 
 __device__ __forceinline__ float other_half(float x, bool maximum) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
@@ -725,12 +738,12 @@ template <int F, int DH, int NW> struct Stage {
         const int key = c / KROW;
         row = lds + key * (DH * 2);
         at = c % KROW * (2 / SZ);
-        turn = key_turn(key) & (DH / 8 - 1);
+        turn = turn_of<DH / 8>(key);
       } else {
         const int ch = (c - KC) / VROW;
         row = lds + KB + ch * (kKeys * 2);
         at = (c - KC) % VROW * (2 / SZ);
-        turn = ch & 7;
+        turn = turn_of<kKeys / 8>(ch);
       }
       if constexpr (is_coded(F)) {
 #pragma unroll
@@ -768,6 +781,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   const int per = max((bl.count + a.n_split - 1) / a.n_split, 1);
   const int v0 = min(split * per, bl.count), v1 = min(v0 + per, bl.count);
   const int ps = a.cache.page_shift;
+  Pages pages;
+  pages.load(a, bl, seq, v0, 1);
 
   const int row = min(wh.base + w * 32 + lr, wh.rows - 1), tok = row / a.group, head = h * a.group + row - tok * a.group;
   const int pos = wh.start + tok;
@@ -808,12 +823,12 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
     for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
   float m = -kInf, l = 0.f;
 
-  const int krow = key_row(lr) * (DH * 2), kturn = (key_turn(key_row(lr)) & (DH / 8 - 1)) ^ half;
-  const int vrow = S::KB + lr * (kKeys * 2), vturn = (lr & 7) ^ half;
+  const int krow = key_row(lr) * (DH * 2), kturn = turn_of<DH / 8>(key_row(lr)) ^ half;
+  const int vrow = S::KB + lr * (kKeys * 2), vturn = turn_of<kKeys / 8>(lr) ^ half;
   S next;
-  const auto fetch = [&](int kb) {
-    const int slot = kb & ((1 << ps) - 1);
-    const int64_t b = (int64_t)page_of(a.rows, a.cache, seq, kb >> ps) * a.cache.n_kv_heads + h;
+  const auto fetch = [&](int v) {
+    const int kb = bl.at(v) * kKeys, slot = kb & ((1 << ps) - 1);
+    const int64_t b = (int64_t)pages.at(v - v0) * a.cache.n_kv_heads + h;
     next.load(reinterpret_cast<const char*>(a.cache.k) + ((b << ps) + slot) * (DH * S::SZ),
               reinterpret_cast<const char*>(a.cache.v) + (((b * DH) << ps) + slot) * S::SZ, ps,
               is_coded(F) ? a.cache.ks + (b << ps) + slot : nullptr, is_coded(F) ? a.cache.vs + (b << ps) + slot : nullptr);
@@ -823,7 +838,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
     next.store(stage[slot], scales[is_coded(F) ? slot : 0], wh.ctx - kb, !sees_all(a, wh, kb), &bad[v & 3]);
   };
   if (v0 < v1) {
-    fetch(bl.at(v0) * kKeys);
+    fetch(v0);
     if (threadIdx.x < 4) bad[threadIdx.x] = 0;
     __syncthreads();
     put(v0, 0);
@@ -833,7 +848,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
     const char* lds = stage[slot];
     __syncthreads();  // this block lies in LDS, and the block before is done with
     if (threadIdx.x == 0) bad[(v + 2) & 3] = 0;
-    if (v + 1 < v1) fetch(bl.at(v + 1) * kKeys);
+    if (((v + 1 - v0) & 63) == 0) pages.load(a, bl, seq, v + 1, 1);
+    if (v + 1 < v1) fetch(v + 1);
     const bool any = kb < ww.prefix || ((!a.causal || kb <= ww.p_last) &&
                      (!a.window || (kb < ww.p_last + a.window && kb + kKeys > ww.p_first - a.window + 1)));
     if (any) {
