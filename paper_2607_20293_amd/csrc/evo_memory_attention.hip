@@ -18,6 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "evo.h"
 #include "evo_memory.hpp"
@@ -33,6 +34,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kKeys = 64;     // keys of a block
 constexpr int kWaves = 4;
+constexpr int kRing = 6;      // operands of a long chunk's products on their way from LDS
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
 
@@ -682,94 +684,108 @@ __device__ __forceinline__ float other_half(float x, bool maximum) {
   return maximum ? fmaxf(a0, a1) : a0 + a1;
 }
 
-// One block on its way from memory to LDS.
+// Blocks on their way from memory to LDS: a thread's chunks of a block's keys
+// and of a block's values.
 template <int F, int DH, int NW> struct Stage {
   static constexpr int SZ = size_of(F), TH = NW * 64;
-  static constexpr int KC = kKeys * DH * SZ / 16;       // 16-byte chunks of keys, as many of values
-  static constexpr int IT = (2 * KC + TH - 1) / TH;
+  static constexpr int KC = kKeys * DH * SZ / 16;       // 16-byte chunks of a block's keys, as many of its values
+  static constexpr int IT = (KC + TH - 1) / TH;
   static constexpr int KROW = DH * SZ / 16, VROW = kKeys * SZ / 16;
-  static constexpr int KB = kKeys * DH * 2, BYTES = 2 * KB;
-  u32x4 w[IT];
+  static constexpr int KB = kKeys * DH * 2;             // bytes of a block's keys in LDS
+  u32x4 k[IT], v[IT];
   float scale;
 
-  // the block's keys and values start at kp and vp, value rows 1 << ps slots apart
-  __device__ __forceinline__ void load(const char* kp, const char* vp, int ps, const float* ks, const float* vs) {
+  // values are dealt from the other end, so that few chunks still meet all waves
+  __device__ __forceinline__ static int key_chunk(int i) { return i * TH + (int)threadIdx.x; }
+  __device__ __forceinline__ static int value_chunk(int i) { return i * TH + ((int)threadIdx.x ^ (TH / 2)); }
+
+  __device__ __forceinline__ void load_keys(const char* p, const float* ks, const float* vs) {
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      const int c = i * TH + (int)threadIdx.x;
-      if (2 * KC % TH && c >= 2 * KC) break;
-      if (c < KC) w[i] = *reinterpret_cast<const u32x4*>(kp + c * 16);
-      else w[i] = *reinterpret_cast<const u32x4*>(vp + ((size_t)(uint32_t)((c - KC) / VROW) << ps) * SZ + (c - KC) % VROW * 16);
-    }
-    if constexpr (is_coded(F)) scale = threadIdx.x < 128 ? (threadIdx.x < 64 ? ks : vs - 64)[threadIdx.x] : 0.f;
+    for (int i = 0; i < IT; ++i)
+      if (KC % TH == 0 || key_chunk(i) < KC) k[i] = *reinterpret_cast<const u32x4*>(p + key_chunk(i) * 16);
+    if constexpr (is_coded(F))
+      if (threadIdx.x < 128) scale = (threadIdx.x < 64 ? ks : vs - 64)[threadIdx.x];
   }
-  // left: keys of the block that the cache holds; values past it become 0.
-  // check: some row does not see all of the block; NaNs and infinities among
-  // its values become 0 then, and *bad is set.
-  __device__ __forceinline__ void store(char* lds, float* scales, int left, bool check, int* bad) const {
+  // value rows lie 1 << ps slots apart
+  __device__ __forceinline__ void load_values(const char* p, int ps) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = i * TH + (int)threadIdx.x;
-      if (2 * KC % TH && c >= 2 * KC) break;
-      u32x4 x = w[i];
-      if (c >= KC && left < kKeys) {
-        const int key = (c - KC) % VROW * (16 / SZ);
+      const int c = value_chunk(i);
+      if (KC % TH == 0 || c < KC) v[i] = *reinterpret_cast<const u32x4*>(p + ((size_t)(uint32_t)(c / VROW) << ps) * SZ + c % VROW * 16);
+    }
+  }
+  __device__ __forceinline__ static void put(char* row, int at, int turn, u32x4 x) {
+    if constexpr (is_coded(F)) {
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+      for (int b = 0; b < 2; ++b) {
+        const u32x2 lo = codes_bf16<F>(x[2 * b]), hi = codes_bf16<F>(x[2 * b + 1]);
+        *reinterpret_cast<u32x4*>(row + ((2 * at + b) ^ turn) * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+      }
+    } else {
+      *reinterpret_cast<u32x4*>(row + (at ^ turn) * 16) = x;
+    }
+  }
+  __device__ __forceinline__ void store_keys(char* lds, float* scales) const {
 #pragma unroll
-          for (int e = 0; e < 4 / SZ; ++e)
-            if (key + d * (4 / SZ) + e >= left) x[d] &= ~(((1u << (8 * SZ)) - 1) << (8 * SZ * e));
-      }
-      if constexpr (F != EVO_CACHE_INT8) {
-        if (check && c >= KC) {
-          bool found = false;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const uint32_t y = finite_only<F>(x[d]);
-            found |= y != x[d];
-            x[d] = y;
-          }
-          if (found) *bad = 1;
-        }
-      }
-      char* row;
-      int at, turn;
-      if (c < KC) {
-        const int key = c / KROW;
-        row = lds + key * (DH * 2);
-        at = c % KROW * (2 / SZ);
-        turn = turn_of<DH / 8>(key);
-      } else {
-        const int ch = (c - KC) / VROW;
-        row = lds + KB + ch * (kKeys * 2);
-        at = (c - KC) % VROW * (2 / SZ);
-        turn = turn_of<kKeys / 8>(ch);
-      }
-      if constexpr (is_coded(F)) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const u32x2 lo = codes_bf16<F>(x[2 * b]), hi = codes_bf16<F>(x[2 * b + 1]);
-          *reinterpret_cast<u32x4*>(row + ((at + b) ^ turn) * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
-        }
-      } else {
-        *reinterpret_cast<u32x4*>(row + (at ^ turn) * 16) = x;
-      }
+    for (int i = 0; i < IT; ++i) {
+      const int c = key_chunk(i), key = c / KROW;
+      if (KC % TH == 0 || c < KC) put(lds + key * (DH * 2), c % KROW, turn_of<DH / 8>(key), k[i]);
     }
     if constexpr (is_coded(F))
       if (threadIdx.x < 128) scales[threadIdx.x] = scale;
   }
+  // left: keys of the block that the cache holds; values past it become 0.
+  // check: some row does not see all of the block; NaNs and infinities among
+  // its values become 0 then, and *bad is set.
+  __device__ __forceinline__ void store_values(char* lds, int left, bool check, int* bad) const {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int c = value_chunk(i), ch = c / VROW;
+      if (KC % TH && c >= KC) continue;
+      u32x4 x = v[i];
+      if (check) {
+        const int key = c % VROW * (16 / SZ);
+        bool found = false;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+#pragma unroll
+          for (int e = 0; e < 4 / SZ; ++e)
+            if (key + d * (4 / SZ) + e >= left) x[d] &= ~(((1u << (8 * SZ)) - 1) << (8 * SZ * e));
+          if constexpr (F != EVO_CACHE_INT8) {
+            const uint32_t y = finite_only<F>(x[d]);
+            found |= y != x[d];
+            x[d] = y;
+          }
+        }
+        if (found) *bad = 1;
+      }
+      put(lds + ch * (kKeys * 2), c % VROW, turn_of<kKeys / 8>(ch), x);
+    }
+  }
 };
 
 // Workgroup (row tile of 32 NW rows, key/value head, part of the keys).
+//
+// Half of the waves run half a block behind the others: while one half of them
+// multiplies (the scores of block i, then the outputs of block i - 1), the other
+// does the softmax of its scores, with a barrier between the halves of a block.
+// Waves w and w + NW / 2 share a SIMD where NW is 8, so that its matrix and
+// vector units work side by side.  In units of barriers, wave half `late` (0 or
+// 1) multiplies for block i at 2 i + late and takes its softmax at 2 i + 1 +
+// late.  There it also stores its share of the keys of block i + 1 + late and
+// of the values of block i + late: both places were last read at 2 i - 1 + 2
+// late at most, and are first read at 2 i + 2 + 2 late.
 template <int F, int DH, int NW>
 __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   typedef Stage<F, DH, NW> S;
   constexpr int TR = 32 * NW, CT = DH / 32;
-  __shared__ __attribute__((aligned(16))) char stage[2][S::BYTES];
+  __shared__ __attribute__((aligned(16))) char lds_k[2][S::KB], lds_v[2][S::KB];
   __shared__ __attribute__((aligned(16))) float scales[is_coded(F) ? 2 : 1][is_coded(F) ? 128 : 1];
-  __shared__ int bad[4];  // of block v at v & 3: cleared two blocks ahead, so that a barrier lies on either side
+  // of the values of block i at i & 3; cleared at 2 i - 4, set at 2 i and 2 i +
+  // 1, read at 2 i + 2 and 2 i + 3
+  __shared__ int bad[4];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lr = lane & 31, half = lane >> 5;
+  const int lr = lane & 31, half = lane >> 5, late = w >= NW / 2 ? 1 : 0;
   // heads fastest, so that a head's row tiles meet on few dies and share their
   // caches; then the parts; the last row tiles, which see most, first
   const int h = blockIdx.x % a.cache.n_kv_heads, rest = blockIdx.x / a.cache.n_kv_heads;
@@ -779,10 +795,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   if (!find_tile(a, tile, TR, &seq, &wh)) return;
   const Blocks bl = blocks_of(a, wh);
   const int per = max((bl.count + a.n_split - 1) / a.n_split, 1);
-  const int v0 = min(split * per, bl.count), v1 = min(v0 + per, bl.count);
+  const int v0 = min(split * per, bl.count), n = min(v0 + per, bl.count) - v0;
   const int ps = a.cache.page_shift;
-  Pages pages;
-  pages.load(a, bl, seq, v0, 1);
 
   const int row = min(wh.base + w * 32 + lr, wh.rows - 1), tok = row / a.group, head = h * a.group + row - tok * a.group;
   const int pos = wh.start + tok;
@@ -824,60 +838,144 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   float m = -kInf, l = 0.f;
 
   const int krow = key_row(lr) * (DH * 2), kturn = turn_of<DH / 8>(key_row(lr)) ^ half;
-  const int vrow = S::KB + lr * (kKeys * 2), vturn = turn_of<kKeys / 8>(lr) ^ half;
+  const int vrow = lr * (kKeys * 2), vturn = turn_of<kKeys / 8>(lr) ^ half;
+
   S next;
-  const auto fetch = [&](int v) {
-    const int kb = bl.at(v) * kKeys, slot = kb & ((1 << ps) - 1);
-    const int64_t b = (int64_t)pages.at(v - v0) * a.cache.n_kv_heads + h;
-    next.load(reinterpret_cast<const char*>(a.cache.k) + ((b << ps) + slot) * (DH * S::SZ),
-              reinterpret_cast<const char*>(a.cache.v) + (((b * DH) << ps) + slot) * S::SZ, ps,
-              is_coded(F) ? a.cache.ks + (b << ps) + slot : nullptr, is_coded(F) ? a.cache.vs + (b << ps) + slot : nullptr);
+  Pages pages;  // of blocks 64 j .. 64 j + 63 of this part, j from the block last asked for
+  int held = 0;
+  pages.load(a, bl, seq, v0, 1);
+  const auto page = [&](int i) {
+    if ((i ^ held) >> 6) {
+      held = i;
+      pages.load(a, bl, seq, v0 + (i & ~63), 1);
+    }
+    return (int64_t)pages.at(i) * a.cache.n_kv_heads + h;
   };
-  const auto put = [&](int v, int slot) {
-    const int kb = bl.at(v) * kKeys;
-    next.store(stage[slot], scales[is_coded(F) ? slot : 0], wh.ctx - kb, !sees_all(a, wh, kb), &bad[v & 3]);
+  const auto fetch_keys = [&](int i) {
+    if (i >= n) return;
+    const int64_t b = (page(i) << ps) + (bl.at(v0 + i) * kKeys & ((1 << ps) - 1));
+    next.load_keys(reinterpret_cast<const char*>(a.cache.k) + b * (DH * S::SZ), is_coded(F) ? a.cache.ks + b : nullptr,
+                   is_coded(F) ? a.cache.vs + b : nullptr);
   };
-  if (v0 < v1) {
-    fetch(v0);
-    if (threadIdx.x < 4) bad[threadIdx.x] = 0;
-    __syncthreads();
-    put(v0, 0);
+  const auto fetch_values = [&](int i) {
+    if (i >= n) return;
+    const int64_t b = ((page(i) * DH) << ps) + (bl.at(v0 + i) * kKeys & ((1 << ps) - 1));
+    next.load_values(reinterpret_cast<const char*>(a.cache.v) + b * S::SZ, ps);
+  };
+  const auto put_keys = [&](int i) {
+    if (i < n) next.store_keys(lds_k[i & 1], scales[is_coded(F) ? i & 1 : 0]);
+  };
+  const auto put_values = [&](int i) {
+    if (i >= n) return;
+    const int kb = bl.at(v0 + i) * kKeys;
+    next.store_values(lds_v[i & 1], wh.ctx - kb, !sees_all(a, wh, kb), &bad[i & 3]);
+  };
+
+  // (values that no terms meet yet, finite all the same)
+  for (int x = threadIdx.x * 16; x < S::KB; x += NW * 64 * 16) *reinterpret_cast<u32x4*>(lds_v[1] + x) = u32x4{0, 0, 0, 0};
+  if (threadIdx.x < 4) bad[threadIdx.x] = 0;
+  __syncthreads();
+  fetch_keys(0);
+  put_keys(0);
+  if (late) {
+    fetch_values(0);
+    fetch_keys(1);
+    put_values(0);
+    put_keys(1);
   }
-  for (int v = v0; v < v1; ++v) {
-    const int kb = bl.at(v) * kKeys, slot = (v - v0) & 1;
-    const char* lds = stage[slot];
-    __syncthreads();  // this block lies in LDS, and the block before is done with
-    if (threadIdx.x == 0) bad[(v + 2) & 3] = 0;
-    if (((v + 1 - v0) & 63) == 0) pages.load(a, bl, seq, v + 1, 1);
-    if (v + 1 < v1) fetch(v + 1);
-    const bool any = kb < ww.prefix || ((!a.causal || kb <= ww.p_last) &&
-                     (!a.window || (kb < ww.p_last + a.window && kb + kKeys > ww.p_first - a.window + 1)));
+  fetch_values(late);
+  fetch_keys(1 + late);
+  __syncthreads();
+  if (late) __syncthreads();
+
+  // The products of a block: its scores, and the outputs of the block before.
+  // kRing operands are on their way from LDS at any time; left to itself the
+  // compiler keeps one, and every matrix instruction waits for its read.
+  // (Always both, also where the terms are zeros or the scores of no use: a
+  // second path would cost a second set of accumulators, and the other half of
+  // the waves would be waited for all the same.)
+  const auto products = [&](f32x16(&s)[2], const bf16x8(&p)[4], const char* keys, const char* values) {
+    constexpr int NK = DH / 8, N = NK + 4 * CT;
+    const auto read = [&](int x) {
+      if (x < NK) return *reinterpret_cast<const bf16x8*>(keys + krow + (x & 1) * (32 * DH * 2) + (((x & ~1) ^ kturn) * 16));
+      const int y = x - NK;
+      return *reinterpret_cast<const bf16x8*>(values + vrow + y % CT * (32 * kKeys * 2) + (((2 * (y / CT)) ^ vturn) * 16));
+    };
+    bf16x8 ring[kRing];
+#pragma unroll
+    for (int x = 0; x < kRing; ++x) ring[x] = read(x);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      if (x < NK) s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[x % kRing], q[x / 2], s[x & 1], 0, 0, 0);
+      else o[(x - NK) % CT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[x % kRing], p[(x - NK) / CT], o[(x - NK) % CT], 0, 0, 0);
+      if (x + kRing < N) ring[x % kRing] = read(x + kRing);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  bf16x8 p[4];  // the terms of the block before
+#pragma unroll
+  for (int j = 0; j < 4; ++j) p[j] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+  for (int i = 0; i <= n; ++i) {
+    const int kb = i < n ? bl.at(v0 + i) * kKeys : 0;
+    const bool any = i < n && (kb < ww.prefix || ((!a.causal || kb <= ww.p_last) &&
+                     (!a.window || (kb < ww.p_last + a.window && kb + kKeys > ww.p_first - a.window + 1))));
+    if (late == 0 && threadIdx.x == 0) bad[(i + 2) & 3] = 0;
+    // ---- products ----
+    __builtin_amdgcn_s_setprio(1);
+    f32x16 s[2];
+    products(s, p, lds_k[i & 1], lds_v[(i - 1) & 1]);
+    if (i > 0) {
+      if constexpr (F != EVO_CACHE_INT8) {
+        if (__builtin_expect(bad[(i - 1) & 3], 0)) {
+          // the values that store_values() took out, for the rows that see them
+          const int kl = bl.at(v0 + i - 1) * kKeys, s0 = kl & ((1 << ps) - 1);
+          const int64_t b = (int64_t)page_of(a.rows, a.cache, seq, kl >> ps) * a.cache.n_kv_heads + h;
+#pragma unroll 1
+          for (int j = 0; j < min(kKeys, wh.ctx - kl); ++j) {
+            const bool see = sees(a, wh, pos, kl + j);
+            int64_t at = ((b * DH + 4 * half) << ps) + s0 + j;
+            asm volatile("" : "+v"(at));  // 64 addresses are made here, not kept over the loop
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float x = not_finite<F>(a.cache.v, at + ((c * 32 + 8 * (e >> 2) + (e & 3)) << ps));
+                if (see) o[c][e] += x;
+                __builtin_amdgcn_sched_barrier(0);
+              }
+          }
+        }
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
+    if (i == n) break;
+    __syncthreads();
+    // ---- softmax, and the next blocks ----
+    put_values(i + late);
+    put_keys(i + 1 + late);
+    fetch_values(i + 1 + late);
+    fetch_keys(i + 2 + late);
     if (any) {
       const bool masked = !sees_all(a, ww, kb);
-      f32x16 s[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
-#pragma unroll
-      for (int k = 0; k < DH / 16; ++k)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const bf16x8 x = *reinterpret_cast<const bf16x8*>(lds + krow + t * (32 * DH * 2) + (((2 * k) ^ kturn) * 16));
-          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[k], s[t], 0, 0, 0);
-        }
       // element e of tile t is key 32 t + 16 (e / 8) + 8 half + e % 8
       const auto key_at = [&](int t, int e) { return kb + 32 * t + 16 * (e >> 3) + 8 * half + (e & 7); };
-      if constexpr (is_coded(F)) {
+      const auto times = [&](const float* by) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(&scales[slot][32 * t + 16 * (e >> 3) + 8 * half + (e & 7)]);
+            const f32x4 x = *reinterpret_cast<const f32x4*>(by + 32 * t + 16 * (e >> 3) + 8 * half + (e & 7));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[t][e + i] *= x[i];
+            for (int d = 0; d < 4; ++d) s[t][e + d] *= x[d];
           }
-      }
+      };
+      if constexpr (is_coded(F)) times(scales[i & 1]);
       if (!plain) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -923,14 +1021,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
         }
       l += sum;
       if constexpr (is_coded(F)) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(&scales[slot][64 + 32 * t + 16 * (e >> 3) + 8 * half + (e & 7)]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[t][e + i] *= x[i];
-          }
+        times(scales[i & 1] + 64);
         if (masked) {
 #pragma unroll
           for (int t = 0; t < 2; ++t)
@@ -939,7 +1030,6 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
               if (!sees(a, wh, pos, key_at(t, e))) s[t][e] = 0.f;
         }
       }
-      bf16x8 p[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         u32x4 x;
@@ -947,37 +1037,13 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
         for (int e = 0; e < 4; ++e) x[e] = pack2(s[j >> 1][(j & 1) * 8 + 2 * e], s[j >> 1][(j & 1) * 8 + 2 * e + 1]);
         p[j] = __builtin_bit_cast(bf16x8, x);
       }
+    } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) {
-          const bf16x8 x = *reinterpret_cast<const bf16x8*>(lds + vrow + c * (32 * kKeys * 2) + (((2 * j) ^ vturn) * 16));
-          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[j], o[c], 0, 0, 0);
-        }
-      if constexpr (F != EVO_CACHE_INT8) {
-        if (__builtin_expect(bad[v & 3], 0)) {
-          // the values that store() took out, for the rows that see them
-          const int s0 = kb & ((1 << ps) - 1);
-          const int64_t b = (int64_t)page_of(a.rows, a.cache, seq, kb >> ps) * a.cache.n_kv_heads + h;
-#pragma unroll 1
-          for (int j = 0; j < min(kKeys, wh.ctx - kb); ++j) {
-            const bool see = sees(a, wh, pos, kb + j);
-            int64_t at = ((b * DH + 4 * half) << ps) + s0 + j;
-            asm volatile("" : "+v"(at));  // 64 addresses are made here, not kept over the loop
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float x = not_finite<F>(a.cache.v, at + ((c * 32 + 8 * (e >> 2) + (e & 3)) << ps));
-                if (see) o[c][e] += x;
-                __builtin_amdgcn_sched_barrier(0);
-              }
-          }
-        }
-      }
+      for (int j = 0; j < 4; ++j) p[j] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
     }
-    if (v + 1 < v1) put(v + 1, slot ^ 1);
+    __syncthreads();
   }
+  if (!late) __syncthreads();  // (as many barriers in both halves)
 
   l = other_half(l, false);
   const int r = w * 32 + lr;
@@ -988,7 +1054,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
       a.part_ml[part * 2] = m;
       a.part_ml[part * 2 + 1] = l;
     }
-    if (v0 >= v1) return;
+    if (n <= 0) return;
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
