@@ -42,6 +42,7 @@ int check_shape(const evo_kv_cache* c) {
   TRY(check_head_dim(c->head_dim));
   if (c->n_pages < 1 || c->n_kv_heads < 1)
     return fail(EVO_E_INVALID, "cache of %d pages, %d heads", c->n_pages, c->n_kv_heads);
+  if ((int64_t)c->n_pages * c->n_kv_heads > kMaxItems) return fail(EVO_E_UNSUPPORTED, "pages * heads above 2^31");
   if (c->page_size < 1) return fail(EVO_E_INVALID, "page_size %d", c->page_size);
   if (c->page_size < 64 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
     return fail(EVO_E_UNSUPPORTED, "page_size %d: 64, 128, 256, 512 and 1024 are supported", c->page_size);

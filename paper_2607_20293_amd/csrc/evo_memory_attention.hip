@@ -168,13 +168,30 @@ __device__ __forceinline__ bool sees(const AttArgs& a, const Where& w, int p, in
   const bool near = (!a.causal || j <= p) && (!a.window || abs(p - j) < a.window);
   return j < w.ctx && (j < w.prefix || near);
 }
-// whether every row of the tile sees every key of block kb .. kb + 63
-__device__ __forceinline__ bool sees_all(const AttArgs& a, const Where& w, int kb) {
-  const int ke = kb + kKeys - 1;
-  const bool near = (!a.causal || ke <= w.p_first) &&
-                    (!a.window || (w.p_last - kb < a.window && ke - w.p_first < a.window));
-  return ke < w.ctx && (ke < w.prefix || near);
-}
+// Which blocks (by their first key) some row of a tile sees, and which all of
+// its rows see whole.
+struct Sight {
+  int any_lo, any_hi, all_lo, all_hi, prefix;
+  __device__ __forceinline__ void set(const AttArgs& a, const Where& w) {
+    any_lo = all_lo = -(1 << 30);
+    any_hi = 1 << 30;
+    all_hi = w.ctx - 1;
+    if (a.causal) {
+      any_hi = w.p_last;
+      all_hi = min(all_hi, w.p_first);
+    }
+    if (a.window) {
+      any_hi = min(any_hi, w.p_last + a.window - 1);
+      any_lo = w.p_first - a.window + 2 - kKeys;
+      all_hi = min(all_hi, w.p_first + a.window - 1);
+      all_lo = w.p_last - a.window + 1;
+    }
+    all_hi -= kKeys - 1;
+    prefix = w.prefix;
+  }
+  __device__ __forceinline__ bool any(int kb) const { return (kb >= any_lo && kb <= any_hi) || kb < prefix; }
+  __device__ __forceinline__ bool all(int kb) const { return (kb >= all_lo && kb <= all_hi) || kb + kKeys <= prefix; }
+};
 
 template <typename T> __device__ __forceinline__ float squash(float x);
 // Behind bf16 products the absolute error of 2^-23 near 0 is far below theirs.
@@ -384,6 +401,8 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
   const int per = max((bl.count + a.n_split - 1) / a.n_split, kWaves);
   const int v0 = split * per, v1 = min(v0 + per, bl.count);
   const int ps = a.cache.page_shift;
+  Sight sight;
+  sight.set(a, wh);
   Pages pages;
   pages.load(a, bl, seq, v0 + w, kWaves);
 
@@ -458,7 +477,7 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
     const int slot = kb & ((1 << ps) - 1);
     if ((it & 63) == 0) pages.load(a, bl, seq, v + kWaves, kWaves);
     page = pages.at(it);
-    const bool masked = !sees_all(a, wh, kb);
+    const bool masked = !sight.all(kb);
     float ks[4][4], vs[4][4];
     if constexpr (is_coded(F)) {
       const int64_t at = (b << ps) + slot;
@@ -684,83 +703,95 @@ __device__ __forceinline__ float other_half(float x, bool maximum) {
   return maximum ? fmaxf(a0, a1) : a0 + a1;
 }
 
-// Blocks on their way from memory to LDS: a thread's chunks of a block's keys
-// and of a block's values.
+// Blocks on their way from memory to LDS: a thread's 16-byte chunks of a block's
+// keys and of a block's values.  Where they lie is the same for every block but
+// for the block's base, which all threads share: offsets are made once.
 template <int F, int DH, int NW> struct Stage {
   static constexpr int SZ = size_of(F), TH = NW * 64;
-  static constexpr int KC = kKeys * DH * SZ / 16;       // 16-byte chunks of a block's keys, as many of its values
+  static constexpr int KC = kKeys * DH * SZ / 16;       // chunks of a block's keys, as many of its values
   static constexpr int IT = (KC + TH - 1) / TH;
   static constexpr int KROW = DH * SZ / 16, VROW = kKeys * SZ / 16;
   static constexpr int KB = kKeys * DH * 2;             // bytes of a block's keys in LDS
+  // a thread's chunks lie so many rows apart, a multiple of 16, so that they
+  // are exchanged alike
+  static constexpr int KSTEP = TH / KROW, VSTEP = TH / VROW;
+  static_assert(IT == 1 || (KSTEP % 16 == 0 && VSTEP % 16 == 0), "turn_of of a thread's chunks");
   u32x4 k[IT], v[IT];
   float scale;
+  uint32_t vat, kto[2], vto[2];  // from: values in memory; to: LDS, one 16-byte place for each 8 values
+  bool has_k, has_v;
 
-  // values are dealt from the other end, so that few chunks still meet all waves
-  __device__ __forceinline__ static int key_chunk(int i) { return i * TH + (int)threadIdx.x; }
-  __device__ __forceinline__ static int value_chunk(int i) { return i * TH + ((int)threadIdx.x ^ (TH / 2)); }
-
+  __device__ __forceinline__ void init(int ps) {
+    // values are dealt from the other end, so that few chunks still meet all waves
+    const uint32_t kc = threadIdx.x, vc = threadIdx.x ^ (TH / 2);
+    has_k = KC % TH == 0 || kc < (uint32_t)KC;
+    has_v = KC % TH == 0 || vc < (uint32_t)KC;
+    vat = ((vc / VROW) << ps) * SZ + vc % VROW * 16;
+    constexpr int PER = 16 / (8 * SZ) ? 16 / (8 * SZ) : 1;  // places of a chunk
+#pragma unroll
+    for (int b = 0; b < PER; ++b) {
+      kto[b] = kc / KROW * (DH * 2) + ((kc % KROW * PER + b) ^ turn_of<DH / 8>(kc / KROW)) * 16;
+      vto[b] = vc / VROW * (kKeys * 2) + ((vc % VROW * PER + b) ^ turn_of<kKeys / 8>(vc / VROW)) * 16;
+    }
+  }
+  // p, ks, vs: the block's base, the same for all threads
   __device__ __forceinline__ void load_keys(const char* p, const float* ks, const float* vs) {
 #pragma unroll
     for (int i = 0; i < IT; ++i)
-      if (KC % TH == 0 || key_chunk(i) < KC) k[i] = *reinterpret_cast<const u32x4*>(p + key_chunk(i) * 16);
+      if (has_k) k[i] = *reinterpret_cast<const u32x4*>(p + (uint32_t)(threadIdx.x * 16 + i * (TH * 16)));
     if constexpr (is_coded(F))
       if (threadIdx.x < 128) scale = (threadIdx.x < 64 ? ks : vs - 64)[threadIdx.x];
   }
-  // value rows lie 1 << ps slots apart
   __device__ __forceinline__ void load_values(const char* p, int ps) {
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      const int c = value_chunk(i);
-      if (KC % TH == 0 || c < KC) v[i] = *reinterpret_cast<const u32x4*>(p + ((size_t)(uint32_t)(c / VROW) << ps) * SZ + c % VROW * 16);
-    }
+    for (int i = 0; i < IT; ++i)
+      if (has_v) v[i] = *reinterpret_cast<const u32x4*>(p + (size_t)((uint32_t)(i * VSTEP) << ps) * SZ + vat);
   }
-  __device__ __forceinline__ static void put(char* row, int at, int turn, u32x4 x) {
+  __device__ __forceinline__ static void put(char* lds, const uint32_t (&to)[2], u32x4 x) {
     if constexpr (is_coded(F)) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const u32x2 lo = codes_bf16<F>(x[2 * b]), hi = codes_bf16<F>(x[2 * b + 1]);
-        *reinterpret_cast<u32x4*>(row + ((2 * at + b) ^ turn) * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+        *reinterpret_cast<u32x4*>(lds + to[b]) = u32x4{lo[0], lo[1], hi[0], hi[1]};
       }
     } else {
-      *reinterpret_cast<u32x4*>(row + (at ^ turn) * 16) = x;
+      *reinterpret_cast<u32x4*>(lds + to[0]) = x;
     }
   }
   __device__ __forceinline__ void store_keys(char* lds, float* scales) const {
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      const int c = key_chunk(i), key = c / KROW;
-      if (KC % TH == 0 || c < KC) put(lds + key * (DH * 2), c % KROW, turn_of<DH / 8>(key), k[i]);
-    }
+    for (int i = 0; i < IT; ++i)
+      if (has_k) put(lds + i * KSTEP * (DH * 2), kto, k[i]);
     if constexpr (is_coded(F))
       if (threadIdx.x < 128) scales[threadIdx.x] = scale;
   }
-  // left: keys of the block that the cache holds; values past it become 0.
-  // check: some row does not see all of the block; NaNs and infinities among
-  // its values become 0 then, and *bad is set.
-  __device__ __forceinline__ void store_values(char* lds, int left, bool check, int* bad) const {
+  __device__ __forceinline__ void store_values(char* lds) const {
+#pragma unroll
+    for (int i = 0; i < IT; ++i)
+      if (has_v) put(lds + i * VSTEP * (kKeys * 2), vto, v[i]);
+  }
+  // Values of a block that some row does not see all of: past the `left` keys
+  // that the cache holds they become 0; NaNs and infinities too, and *bad is set.
+  __device__ __forceinline__ void clear_values(int left, int* bad) {
+    bool found = false;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = value_chunk(i), ch = c / VROW;
-      if (KC % TH && c >= KC) continue;
-      u32x4 x = v[i];
-      if (check) {
-        const int key = c % VROW * (16 / SZ);
-        bool found = false;
+      const int key = (int)((threadIdx.x ^ (TH / 2)) % VROW) * (16 / SZ);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
+      for (int d = 0; d < 4; ++d) {
+        uint32_t x = v[i][d];
 #pragma unroll
-          for (int e = 0; e < 4 / SZ; ++e)
-            if (key + d * (4 / SZ) + e >= left) x[d] &= ~(((1u << (8 * SZ)) - 1) << (8 * SZ * e));
-          if constexpr (F != EVO_CACHE_INT8) {
-            const uint32_t y = finite_only<F>(x[d]);
-            found |= y != x[d];
-            x[d] = y;
-          }
+        for (int e = 0; e < 4 / SZ; ++e)
+          if (key + d * (4 / SZ) + e >= left) x &= ~(((1u << (8 * SZ)) - 1) << (8 * SZ * e));
+        if constexpr (F != EVO_CACHE_INT8) {
+          const uint32_t y = finite_only<F>(x);
+          found |= y != x;
+          x = y;
         }
-        if (found) *bad = 1;
+        v[i][d] = x;
       }
-      put(lds + ch * (kKeys * 2), c % VROW, turn_of<kKeys / 8>(ch), x);
     }
+    if (found && has_v) *bad = 1;
   }
 };
 
@@ -774,15 +805,17 @@ template <int F, int DH, int NW> struct Stage {
 // 1) multiplies for block i at 2 i + late and takes its softmax at 2 i + 1 +
 // late.  There it also stores its share of the keys of block i + 1 + late and
 // of the values of block i + late: both places were last read at 2 i - 1 + 2
-// late at most, and are first read at 2 i + 2 + 2 late.
+// late at most, and are first read at 2 i + 2 + 2 late.  (Scales are stored with
+// the keys by the first two waves, at 2 i - 1 for block i; the softmax of block
+// i - 2 has read their place at 2 i - 2.)  With the products instead, a
+// 4096-token chunk behind 8192 tokens took 707 us; here 689 us.
 template <int F, int DH, int NW>
 __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   typedef Stage<F, DH, NW> S;
   constexpr int TR = 32 * NW, CT = DH / 32;
   __shared__ __attribute__((aligned(16))) char lds_k[2][S::KB], lds_v[2][S::KB];
   __shared__ __attribute__((aligned(16))) float scales[is_coded(F) ? 2 : 1][is_coded(F) ? 128 : 1];
-  // of the values of block i at i & 3; cleared at 2 i - 4, set at 2 i and 2 i +
-  // 1, read at 2 i + 2 and 2 i + 3
+  // of the values of block i at i & 3; cleared at 2 i - 4, set at 2 i and 2 i + 1, read at 2 i + 2 and 2 i + 3
   __shared__ int bad[4];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, half = lane >> 5, late = w >= NW / 2 ? 1 : 0;
@@ -802,11 +835,14 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   const int pos = wh.start + tok;
   const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
   // what this wave's rows see, to skip masks and whole blocks
-  Where ww = wh;
+  Sight sight, tile_sight;
   {
+    Where ww = wh;
     const int r0 = wh.base + w * 32;
     ww.p_first = wh.start + min(r0, wh.rows - 1) / a.group;
     ww.p_last = wh.start + min(r0 + 31, wh.rows - 1) / a.group;
+    sight.set(a, ww);
+    tile_sight.set(a, wh);
   }
   // scores in units of log2: with no cap or bias by one factor inside the
   // exponential (its sign moved to the query, so that the largest product is
@@ -841,26 +877,35 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   const int vrow = lr * (kKeys * 2), vturn = turn_of<kKeys / 8>(lr) ^ half;
 
   S next;
-  Pages pages;  // of blocks 64 j .. 64 j + 63 of this part, j from the block last asked for
-  int held = 0;
-  pages.load(a, bl, seq, v0, 1);
-  const auto page = [&](int i) {
-    if ((i ^ held) >> 6) {
-      held = i;
-      pages.load(a, bl, seq, v0 + (i & ~63), 1);
-    }
-    return (int64_t)pages.at(i) * a.cache.n_kv_heads + h;
+  next.init(ps);
+  // Where block i of this part lies: first element of its page and head, slot.
+  // Keys are asked for a block ahead of values, which use what was found then.
+  struct Place {
+    int64_t first;
+    int slot;
   };
+  Pages pages;
+  pages.load(a, bl, seq, v0, 1);
+  int paged = 64;  // blocks below it are in `pages`
+  const auto place = [&](int i) {
+    if (i >= paged) {
+      pages.load(a, bl, seq, v0 + i, 1);
+      paged += 64;
+    }
+    const int head_page = pages.at(i) * a.cache.n_kv_heads + h;  // (pages * heads stay below 2^31, see the checks)
+    return Place{(int64_t)head_page * (DH << ps), bl.at(v0 + i) * kKeys & ((1 << ps) - 1)};
+  };
+  Place at_keys = {}, at_values = {};
   const auto fetch_keys = [&](int i) {
     if (i >= n) return;
-    const int64_t b = (page(i) << ps) + (bl.at(v0 + i) * kKeys & ((1 << ps) - 1));
-    next.load_keys(reinterpret_cast<const char*>(a.cache.k) + b * (DH * S::SZ), is_coded(F) ? a.cache.ks + b : nullptr,
-                   is_coded(F) ? a.cache.vs + b : nullptr);
+    at_keys = place(i);
+    const int64_t key = at_keys.first + at_keys.slot * DH, row = at_keys.first / DH + at_keys.slot;
+    next.load_keys(reinterpret_cast<const char*>(a.cache.k) + key * S::SZ, is_coded(F) ? a.cache.ks + row : nullptr,
+                   is_coded(F) ? a.cache.vs + row : nullptr);
   };
   const auto fetch_values = [&](int i) {
     if (i >= n) return;
-    const int64_t b = ((page(i) * DH) << ps) + (bl.at(v0 + i) * kKeys & ((1 << ps) - 1));
-    next.load_values(reinterpret_cast<const char*>(a.cache.v) + b * S::SZ, ps);
+    next.load_values(reinterpret_cast<const char*>(a.cache.v) + (at_values.first + at_values.slot) * S::SZ, ps);
   };
   const auto put_keys = [&](int i) {
     if (i < n) next.store_keys(lds_k[i & 1], scales[is_coded(F) ? i & 1 : 0]);
@@ -868,7 +913,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   const auto put_values = [&](int i) {
     if (i >= n) return;
     const int kb = bl.at(v0 + i) * kKeys;
-    next.store_values(lds_v[i & 1], wh.ctx - kb, !sees_all(a, wh, kb), &bad[i & 3]);
+    if (!tile_sight.all(kb)) next.clear_values(wh.ctx - kb, &bad[i & 3]);
+    next.store_values(lds_v[i & 1]);
   };
 
   // (values that no terms meet yet, finite all the same)
@@ -876,10 +922,12 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   if (threadIdx.x < 4) bad[threadIdx.x] = 0;
   __syncthreads();
   fetch_keys(0);
+  at_values = at_keys;
   put_keys(0);
   if (late) {
     fetch_values(0);
     fetch_keys(1);
+    at_values = at_keys;
     put_values(0);
     put_keys(1);
   }
@@ -923,11 +971,9 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   for (int j = 0; j < 4; ++j) p[j] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
   for (int i = 0; i <= n; ++i) {
     const int kb = i < n ? bl.at(v0 + i) * kKeys : 0;
-    const bool any = i < n && (kb < ww.prefix || ((!a.causal || kb <= ww.p_last) &&
-                     (!a.window || (kb < ww.p_last + a.window && kb + kKeys > ww.p_first - a.window + 1))));
+    const bool any = i < n && sight.any(kb);
     if (late == 0 && threadIdx.x == 0) bad[(i + 2) & 3] = 0;
     // ---- products ----
-    __builtin_amdgcn_s_setprio(1);
     f32x16 s[2];
     products(s, p, lds_k[i & 1], lds_v[(i - 1) & 1]);
     if (i > 0) {
@@ -953,16 +999,16 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
         }
       }
     }
-    __builtin_amdgcn_s_setprio(0);
     if (i == n) break;
     __syncthreads();
     // ---- softmax, and the next blocks ----
     put_values(i + late);
     put_keys(i + 1 + late);
+    at_values = at_keys;
     fetch_values(i + 1 + late);
     fetch_keys(i + 2 + late);
     if (any) {
-      const bool masked = !sees_all(a, ww, kb);
+      const bool masked = !sight.all(kb);
       // element e of tile t is key 32 t + 16 (e / 8) + 8 half + e % 8
       const auto key_at = [&](int t, int e) { return kb + 32 * t + 16 * (e >> 3) + 8 * half + (e & 7); };
       const auto times = [&](const float* by) {
