@@ -121,7 +121,8 @@ CacheView view(const evo_kv_cache* c) {
 RowsView view(const evo_kv_rows* r) {
   // sequences that are all full need no cu_rows
   const bool full = r->n_rows == (int64_t)r->n_seqs * r->max_rows;
-  return RowsView{full ? nullptr : r->cu_rows, r->page_table, r->n_seqs, r->n_rows, r->max_rows, r->max_pages};
+  return RowsView{full ? nullptr : r->cu_rows, r->page_table, r->n_seqs, r->n_rows, r->max_rows, r->max_pages,
+                  Divisor::of(r->max_rows ? r->max_rows : 1)};
 }
 
 void set_norm_rope(RowsArgs* a, const evo_norm_rope* n) {
@@ -319,7 +320,7 @@ int evo_chunk_attention(const evo_kv_cache* cache, const evo_kv_rows* rows, cons
   const int64_t need = bytes_of(p);
   if (need > 0 && (!workspace || workspace_bytes < (size_t)need || !aligned(workspace, 16)))
     return fail(EVO_E_INVALID, "the workspace must hold %lld bytes, 16-byte aligned", (long long)need);
-  if ((int64_t)p.n_tiles * cache->n_kv_heads * p.n_split > kMaxItems) return fail(EVO_E_UNSUPPORTED, "too many row tiles");
+  if (((int64_t)p.n_tiles * cache->n_kv_heads + 8ll * p.tiles_per_seq) * p.n_split > kMaxItems) return fail(EVO_E_UNSUPPORTED, "too many row tiles");
   a.q = view(q);
   a.out = view(out);
   a.lse = lse;
@@ -338,6 +339,11 @@ int evo_chunk_attention(const evo_kv_cache* cache, const evo_kv_rows* rows, cons
   a.tiles_per_seq = p.tiles_per_seq;
   a.n_tiles = p.n_tiles;
   a.n_split = p.n_split;
+  a.by_group = Divisor::of(a.group);
+  a.by_kv_heads = Divisor::of(cache->n_kv_heads);
+  a.by_tiles = Divisor::of(p.tiles_per_seq ? p.tiles_per_seq : 1);
+  a.by_eight = Divisor::of(8ll * (p.tiles_per_seq ? p.tiles_per_seq : 1));
+  a.by_split = Divisor::of(p.n_split);
   a.part = (float*)workspace;
   a.part_ml = (float*)workspace + p.part_floats;
   return launched(launch_attention(att->dtype, cache->format, cache->head_dim, p, a, (hipStream_t)hip_stream));

@@ -9,6 +9,24 @@
 
 namespace evo {
 
+// Division of n < 2^31 by a divisor that the launch knows, in five operations
+// (T. Granlund and P. Montgomery, Division by invariant integers using
+// multiplication, PLDI 1994): the compiler's own for unknown divisors is some
+// forty, and short calls are mostly such work.
+struct Divisor {
+  uint32_t m;
+  int32_t s1, s2;
+  static Divisor of(int64_t d) {
+    int l = 0;
+    while ((1ll << l) < d) ++l;
+    return Divisor{(uint32_t)((((1ull << l) - (uint64_t)d) << 32) / (uint64_t)d + 1), l < 1 ? l : 1, l < 1 ? 0 : l - 1};
+  }
+  __device__ __forceinline__ int divide(int n) const {
+    const uint32_t t = __umulhi(m, (uint32_t)n);
+    return (int)((t + (((uint32_t)n - t) >> s1)) >> s2);
+  }
+};
+
 // The paged cache (layout: evo.h).  All pages of one head are page_size slots;
 // page_size is 1 << page_shift.
 struct CacheView {
@@ -24,6 +42,7 @@ struct RowsView {
   const int32_t* cu;
   const int32_t* pages;   // [n_seqs][max_pages]
   int n_seqs, n_rows, max_rows, max_pages;
+  Divisor by_max_rows;    // without cu
 };
 
 struct HeadsView {
@@ -48,6 +67,7 @@ struct RowsArgs {
   RowsView rows;
   int wide;                   // every row 16-byte aligned
   int qk_blocks;              // workgroups of the q and k part
+  Divisor by_groups, by_kv_heads;
 };
 
 // format: EVO_CACHE_*, or -1 with no cache (keys to ko).  dtype: EVO_FP32 / EVO_BF16.
@@ -71,6 +91,7 @@ struct AttArgs {
   int tiles_per_seq;          // 0: a sequence's tiles start at row / tile + sequence
   int n_tiles;                // row tiles over all sequences
   int n_split;                // parts of the keys
+  Divisor by_group, by_kv_heads, by_tiles, by_eight, by_split;  // (by_eight: 8 sequences' tiles)
   float* part;                // [n_tiles][n_kv_heads][n_split][tile rows][head_dim] unnormalised outputs
   float* part_ml;             // [n_tiles][n_kv_heads][n_split][tile rows][2]: maximum (log2), sum
 };
@@ -88,7 +109,7 @@ hipError_t launch_attention(int dtype, int format, int head_dim, const AttPlan& 
 // The sequence of row n and the row's place in it.
 __device__ __forceinline__ void find_row(const RowsView& r, int n, int* seq, int* i) {
   if (!r.cu) {
-    const int s = n / r.max_rows;
+    const int s = r.by_max_rows.divide(n);
     *seq = s;
     *i = n - s * r.max_rows;
     return;

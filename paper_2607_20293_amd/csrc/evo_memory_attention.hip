@@ -34,6 +34,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kKeys = 64;     // keys of a block
 constexpr int kWaves = 4;
+// Least blocks of a part of the keys.  A part costs a second launch to join it:
+// one token over 1000 positions took 15.8, 15.6 and 13.4 us with 4, 8 and 16, 200
+// fp32 rows with a window 34.8, 24.4 and 24.4 us.
+constexpr int kPartBlocks = 16;
 constexpr int kRing = 6;      // operands of a long chunk's products on their way from LDS
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
@@ -93,6 +97,28 @@ template <int F, int DH> struct Lay {
   }
 };
 
+// The row tile, key/value head and part of the keys of a workgroup.  The tiles
+// of a sequence read the same keys: they lie 8 workgroups apart, which puts
+// them on one die (workgroup i runs on die i % 8) and its cache; the last, which
+// sees most, comes first.
+__device__ __forceinline__ bool find_unit(const AttArgs& a, int block, int* tile, int* h, int* split) {
+  int unit = block, j = 0;
+  if (a.tiles_per_seq > 1) {
+    const int eight = a.by_eight.divide(block), rest = block - eight * 8 * a.tiles_per_seq;
+    unit = eight * 8 + (rest & 7);
+    j = a.tiles_per_seq - 1 - (rest >> 3);
+  }
+  const int th = a.by_split.divide(unit);
+  *split = unit - th * a.n_split;
+  *tile = a.by_kv_heads.divide(th);
+  *h = th - *tile * a.cache.n_kv_heads;
+  if (a.tiles_per_seq > 1) {
+    if (*tile >= a.rows.n_seqs) return false;
+    *tile = *tile * a.tiles_per_seq + j;
+  }
+  return true;
+}
+
 struct Where {
   int row0, rows, base, p_first, p_last, ctx, start, prefix;
 };
@@ -101,7 +127,7 @@ struct Where {
 __device__ __forceinline__ bool find_tile(const AttArgs& a, int tile, int tile_rows, int* seq_out, Where* w) {
   int seq, j;
   if (a.tiles_per_seq) {
-    seq = tile / a.tiles_per_seq;
+    seq = a.by_tiles.divide(tile);
     j = tile - seq * a.tiles_per_seq;
   } else {
     int lo = 0, hi = a.rows.n_seqs;
@@ -128,8 +154,8 @@ __device__ __forceinline__ bool find_tile(const AttArgs& a, int tile, int tile_r
   w->ctx = min(max(a.lengths[seq], 0), a.rows.max_pages << a.cache.page_shift);
   w->start = a.starts ? min(max(a.starts[seq], -(1 << 29)), 1 << 29) : w->ctx - n;
   w->prefix = a.prefix ? min(max(a.prefix[seq], 0), w->ctx) : 0;
-  w->p_first = w->start + w->base / a.group;
-  w->p_last = w->start + (min(w->base + tile_rows, w->rows) - 1) / a.group;
+  w->p_first = w->start + a.by_group.divide(w->base);
+  w->p_last = w->start + a.by_group.divide(min(w->base + tile_rows, w->rows) - 1);
   *seq_out = seq;
   return true;
 }
@@ -201,8 +227,20 @@ template <> __device__ __forceinline__ float squash<__bf16>(float x) {
 template <> __device__ __forceinline__ float squash<float>(float x) { return tanhf(x); }
 
 template <typename T, int DH> struct Query;
-template <int DH> struct Query<__bf16, DH> { bf16x8 f[DH / 32]; };
-template <int DH> struct Query<float, DH> { float f[DH / 4]; };
+template <int DH> struct Query<__bf16, DH> {
+  bf16x8 f[DH / 32];
+  __device__ __forceinline__ void negate() {
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k) f[k] = -f[k];
+  }
+};
+template <int DH> struct Query<float, DH> {
+  float f[DH / 4];
+  __device__ __forceinline__ void negate() {
+#pragma unroll
+    for (int k = 0; k < DH / 4; ++k) f[k] = -f[k];
+  }
+};
 
 // This lane's share of a query row, in the order of the key loads.
 template <int F, int DH>
@@ -381,7 +419,8 @@ template <typename T> __device__ __forceinline__ void store4(T* p, int wide, f32
 // Workgroup (row tile, key/value head, part of the keys).
 // Waves that a SIMD shall hold: what the registers of a wave's block allow.
 template <typename T> constexpr int waves_per_simd(int f, int dh, int r) {
-  return sizeof(T) == 4 || (dh == 128 && (f == EVO_CACHE_BF16 || r == 2)) ? 1 : r == 2 || dh == 128 ? 2 : 3;
+  if (sizeof(T) == 4) return dh == 128 || (dh == 64 && r == 2) ? 1 : 2;
+  return dh == 128 && f == EVO_CACHE_BF16 ? 1 : r == 2 || dh == 128 ? 2 : 3;
 }
 
 template <typename T, int F, int DH, int R>
@@ -392,13 +431,12 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
   __shared__ float join_ml[kWaves][TR][2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, g = lane >> 4;
-  const int split = blockIdx.x % a.n_split, th = blockIdx.x / a.n_split;
-  const int h = th % a.cache.n_kv_heads, tile = th / a.cache.n_kv_heads;
-  int seq;
+  int tile, h, split, seq;
   Where wh;
-  if (!find_tile(a, tile, TR, &seq, &wh)) return;
+  if (!find_unit(a, blockIdx.x, &tile, &h, &split) || !find_tile(a, tile, TR, &seq, &wh)) return;
+  const int th = tile * a.cache.n_kv_heads + h;
   const Blocks bl = blocks_of(a, wh);
-  const int per = max((bl.count + a.n_split - 1) / a.n_split, kWaves);
+  const int per = max(a.by_split.divide(bl.count + a.n_split - 1), kWaves);
   const int v0 = split * per, v1 = min(v0 + per, bl.count);
   const int ps = a.cache.page_shift;
   Sight sight;
@@ -406,15 +444,28 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
   Pages pages;
   pages.load(a, bl, seq, v0 + w, kWaves);
 
+  // Scores in units of log2 are off + mul x, mul > 0, with x the products by
+  //   plain: one factor, inside the exponential (codes: with the key's scale)
+  //   capped: cap tanh(z / cap) = cap + 2 cap x, x = -1 / (1 + exp(2 z / cap));
+  //     its absolute error of 2^-23 cap is far below that of bf16 products
+  //   else: everything ahead of it
+  const bool capped = sizeof(T) == 2 && a.cap > 0.f && !a.slopes;
+  const bool plain = a.cap == 0.f && !a.slopes && a.scale != 0.f;
+  const float cap_log2 = a.cap * kLog2e, to_log2 = a.scale * kLog2e;
+  const float pre = capped ? 2.f * to_log2 / a.cap : a.cap > 0.f ? a.scale / a.cap : to_log2;
+  const float mul = capped ? 2.f * cap_log2 : plain && !is_coded(F) ? fabsf(to_log2) : 1.f, off = capped ? cap_log2 : 0.f;
+  const bool flip = plain && !is_coded(F) && a.scale < 0.f;
+
   Query<T, DH> q[R];
   int pos[R];
   float slope[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int row = min(wh.base + r * 16 + lr, wh.rows - 1), tok = row / a.group, head = h * a.group + row - tok * a.group;
+    const int row = min(wh.base + r * 16 + lr, wh.rows - 1), tok = a.by_group.divide(row), head = h * a.group + row - tok * a.group;
     pos[r] = wh.start + tok;
     slope[r] = a.slopes ? a.slopes[head] * kLog2e : 0.f;
     load_query<F, DH>(q[r], reinterpret_cast<const T*>(a.q.p) + (wh.row0 + tok) * a.q.row + head * a.q.head, g, a.wide);
+    if (flip) q[r].negate();
   }
   f32x4 o[R][L::CT];
   float m[R], l[R];
@@ -425,7 +476,6 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
 #pragma unroll
     for (int c = 0; c < L::CT; ++c) o[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const float to_log2 = a.scale * kLog2e, to_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, cap_log2 = a.cap * kLog2e;
 
   // byte offsets of this lane in a block's keys and values
   const uint32_t koff = (uint32_t)((L::key_of(0, lr >> 2, lr & 3) * DH + g * L::E) * L::SZ);
@@ -486,7 +536,7 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
         const f32x4 x = *reinterpret_cast<const f32x4*>(a.cache.ks + at + L::key_of(t, g, 0));
         const f32x4 y = *reinterpret_cast<const f32x4*>(a.cache.vs + at + L::key_of(t, g, 0));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { ks[t][i] = x[i]; vs[t][i] = y[i]; }
+        for (int i = 0; i < 4; ++i) { ks[t][i] = x[i] * pre; vs[t][i] = y[i]; }
       }
     }
     f32x4 s[R][4];
@@ -501,70 +551,46 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
     Terms<T> terms[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      float z[4][4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = s[r][t][i];
-          if constexpr (is_coded(F)) x *= ks[t][i];
-          z[t][i] = x;
-        }
-      if (a.cap > 0.f) {
+      float x[4][4];
+      const auto each = [&](auto f) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) z[t][i] = cap_log2 * squash<T>(z[t][i] * to_cap);
-      } else {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) z[t][i] *= to_log2;
+          for (int i = 0; i < 4; ++i) f(x[t][i], t, i);
+      };
+      each([&](float& x, int t, int i) { x = is_coded(F) ? s[r][t][i] * ks[t][i] : s[r][t][i]; });
+      if (capped) {
+        each([&](float& x, int, int) { x = __builtin_amdgcn_rcpf(-1.f - exp2_(is_coded(F) ? x : x * pre)); });
+      } else if (!plain) {
+        if (!is_coded(F)) each([&](float& x, int, int) { x *= pre; });
+        if (a.cap > 0.f) each([&](float& x, int, int) { x = cap_log2 * squash<T>(x); });
+        if (a.slopes)
+          each([&](float& x, int t, int i) { x = fmaf(-slope[r], fabsf((float)(pos[r] - kb - L::key_of(t, g, i))), x); });
       }
-      if (a.slopes) {
+      if (masked) each([&](float& x, int t, int i) { x = sees(a, wh, pos[r], kb + L::key_of(t, g, i)) ? x : -kInf; });
+      float top = x[0][0];
+      each([&](float& x, int, int) { top = fmaxf(top, x); });
+      top = over_groups(fmaf(top, mul, off), true);
+      // the maximum moves only when scores outgrow it by 2^8: terms stay below
+      // 2^8 of the true maximum's, and the outputs are seldom rescaled
+      if (__any(!(top <= m[r] + 8.f))) {
+        const float m_new = fmaxf(m[r], top);
+        const float f = exp2_(m[r] - (m_new == -kInf ? 0.f : m_new));
+        m[r] = m_new;
+        l[r] *= f;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) z[t][i] = fmaf(-slope[r], fabsf((float)(pos[r] - kb - L::key_of(t, g, i))), z[t][i]);
+        for (int c = 0; c < L::CT; ++c) o[r][c] *= f;
       }
-      if (masked) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!sees(a, wh, pos[r], kb + L::key_of(t, g, i))) z[t][i] = -kInf;
-      }
-      float top = z[0][0];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, z[t][i]);
-      top = over_groups(top, true);
-      const float m_new = fmaxf(m[r], top);
-      const float base = m_new == -kInf ? 0.f : m_new;
-      const float f = exp2_(m[r] - base);
-      m[r] = m_new;
+      const float shift = off - (m[r] == -kInf ? 0.f : m[r]);
       float sum = 0.f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          z[t][i] = exp2_(z[t][i] - base);
-          sum += z[t][i];
-        }
-      l[r] = fmaf(l[r], f, sum);
-#pragma unroll
-      for (int c = 0; c < L::CT; ++c) o[r][c] *= f;
+      each([&](float& x, int, int) { x = exp2_(fmaf(x, mul, shift)); sum += x; });
+      l[r] += sum;
       if constexpr (is_coded(F)) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            z[t][i] *= vs[t][i];
-            if (masked && !sees(a, wh, pos[r], kb + L::key_of(t, g, i))) z[t][i] = 0.f;
-          }
+        // (an unseen key's scale may be a NaN)
+        if (masked) each([&](float& x, int t, int i) { x = sees(a, wh, pos[r], kb + L::key_of(t, g, i)) ? x * vs[t][i] : 0.f; });
+        else each([&](float& x, int t, int i) { x *= vs[t][i]; });
       }
-      terms[r].set(z);
+      terms[r].set(x);
     }
     bool bad = false;
     if (masked) {
@@ -642,8 +668,7 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
   if (w >= 2) put(join_o[w - 2]);
   __syncthreads();
   if (w < 2) add(join_o[w]);
-  __syncthreads();
-  if (w == 1) put(join_o[1]);
+  if (w == 1) put(join_o[1]);  // (the place that it has just read)
   __syncthreads();
   if (w != 0) return;
   add(join_o[1]);
@@ -664,7 +689,7 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
       }
       continue;
     }
-    const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+    const int tok = a.by_group.divide(row), head = h * a.group + row - tok * a.group;
     const float inv = total[r] == 0.f ? 0.f : 1.f / total[r];
     T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
 #pragma unroll
@@ -819,19 +844,15 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   __shared__ int bad[4];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, half = lane >> 5, late = w >= NW / 2 ? 1 : 0;
-  // heads fastest, so that a head's row tiles meet on few dies and share their
-  // caches; then the parts; the last row tiles, which see most, first
-  const int h = blockIdx.x % a.cache.n_kv_heads, rest = blockIdx.x / a.cache.n_kv_heads;
-  const int split = rest % a.n_split, tile = a.n_tiles - 1 - rest / a.n_split;
-  int seq;
+  int tile, h, split, seq;
   Where wh;
-  if (!find_tile(a, tile, TR, &seq, &wh)) return;
+  if (!find_unit(a, blockIdx.x, &tile, &h, &split) || !find_tile(a, tile, TR, &seq, &wh)) return;
   const Blocks bl = blocks_of(a, wh);
-  const int per = max((bl.count + a.n_split - 1) / a.n_split, 1);
+  const int per = max(a.by_split.divide(bl.count + a.n_split - 1), 1);
   const int v0 = min(split * per, bl.count), n = min(v0 + per, bl.count) - v0;
   const int ps = a.cache.page_shift;
 
-  const int row = min(wh.base + w * 32 + lr, wh.rows - 1), tok = row / a.group, head = h * a.group + row - tok * a.group;
+  const int row = min(wh.base + w * 32 + lr, wh.rows - 1), tok = a.by_group.divide(row), head = h * a.group + row - tok * a.group;
   const int pos = wh.start + tok;
   const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
   // what this wave's rows see, to skip masks and whole blocks
@@ -839,8 +860,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   {
     Where ww = wh;
     const int r0 = wh.base + w * 32;
-    ww.p_first = wh.start + min(r0, wh.rows - 1) / a.group;
-    ww.p_last = wh.start + min(r0 + 31, wh.rows - 1) / a.group;
+    ww.p_first = wh.start + a.by_group.divide(min(r0, wh.rows - 1));
+    ww.p_last = wh.start + a.by_group.divide(min(r0 + 31, wh.rows - 1));
     sight.set(a, ww);
     tile_sight.set(a, wh);
   }
@@ -1127,7 +1148,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
   constexpr int AT = 8;
   const int x = (blockIdx.x * 256 + threadIdx.x) % (tile_rows * (DH / 4));
   const int th = (blockIdx.x * 256 + threadIdx.x) / (tile_rows * (DH / 4));
-  const int h = th % a.cache.n_kv_heads, tile = th / a.cache.n_kv_heads;
+  const int tile = a.by_kv_heads.divide(th), h = th - tile * a.cache.n_kv_heads;
   int seq;
   Where wh;
   if (tile >= a.n_tiles || !find_tile(a, tile, tile_rows, &seq, &wh)) return;
@@ -1161,7 +1182,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
       o += v[i] * f;
     }
   }
-  const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+  const int tok = a.by_group.divide(row), head = h * a.group + row - tok * a.group;
   T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
   store4(dst + c, a.wide, t == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / t));
   if (a.lse && c == 0)
@@ -1171,22 +1192,41 @@ __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
 template <typename T, int F, int DH>
 hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
   const int64_t blocks = (int64_t)p.n_tiles * a.cache.n_kv_heads;
-  if (p.tile_rows > 32) {
-    if constexpr (sizeof(T) == 2) {
-      if (p.tile_rows == 128)
-        hipLaunchKernelGGL((tile_kernel<F, DH, 4>), dim3(blocks * p.n_split), dim3(256), 0, stream, a);
-      else
-        hipLaunchKernelGGL((tile_kernel<F, DH, 8>), dim3(blocks * p.n_split), dim3(512), 0, stream, a);
-    }
-  } else if (p.tile_rows == 16)
-    hipLaunchKernelGGL((stream_kernel<T, F, DH, 1>), dim3(blocks * p.n_split), dim3(kWaves * 64), 0, stream, a);
-  else if constexpr (!(F == EVO_CACHE_FP32 && DH == 128))
-    hipLaunchKernelGGL((stream_kernel<T, F, DH, 2>), dim3(blocks * p.n_split), dim3(kWaves * 64), 0, stream, a);
+  int64_t wgs = blocks * p.n_split;
+  if (p.tiles_per_seq > 1) wgs = (wgs / p.tiles_per_seq + 7) / 8 * 8 * p.tiles_per_seq;  // (see find_unit)
+  if (p.tile_rows == 16) {
+    hipLaunchKernelGGL((stream_kernel<T, F, DH, 1>), dim3(wgs), dim3(kWaves * 64), 0, stream, a);
+  } else if (p.tile_rows == 32) {
+    if constexpr (!is_coded(F) && !(F == EVO_CACHE_FP32 && DH == 128))
+      hipLaunchKernelGGL((stream_kernel<T, F, DH, 2>), dim3(wgs), dim3(kWaves * 64), 0, stream, a);
+  } else if constexpr (sizeof(T) == 2) {
+    if (p.tile_rows == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 4>), dim3(wgs), dim3(256), 0, stream, a);
+    else if constexpr (DH == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 8>), dim3(wgs), dim3(512), 0, stream, a);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_split == 1) return e;
   hipLaunchKernelGGL((join_kernel<T, DH>), dim3((blocks * p.tile_rows * (DH / 4) + 255) / 256), dim3(256), 0, stream, a,
                      p.tile_rows);
   return hipGetLastError();
+}
+
+// Rows of a tile, by the rows that a sequence has for a key/value head.
+// Measured, us of a call (12 heads of 64 over 4000 positions of 16 sequences, or 8
+// heads of 128, grouped by four, over 8000):
+//  * 8-bit caches take 16 rows to a wave up to 128: the registers then hold
+//    three waves to a SIMD, which hide the conversions.  32 rows 34 (two row
+//    blocks to a wave 39), 64 rows 52 (63; through LDS 87), 100 rows 73 (LDS
+//    92); 200 rows of 8 sequences 70 and 73.
+//  * others take two row blocks, which halves the reads: 32 rows 35 (one 47), 64
+//    rows 57 (one 85, LDS 64); heads of 128: 32 rows 89 (129, LDS 95), 64 rows
+//    130 (181, LDS 81).  Two row blocks of fp32 keys of 128 do not fit.
+//  * through LDS, heads of 128 take tiles of 256 (4096 rows behind 8192 659,
+//    tiles of 128 746; 64 rows, 256 to a head, 76 and 85), the others of 128
+//    (1024 rows behind 1024, 4 sequences, 51, tiles of 256 59; int8 75 and 93).
+int tile_rows_of(int dtype, int format, int head_dim, int64_t rows) {
+  const bool lds = dtype == EVO_BF16 && rows > (is_coded(format) ? 128 : head_dim == 128 ? 32 : 64);
+  if (lds) return head_dim == 128 && rows > 128 ? 256 : 128;
+  return rows <= 16 || is_coded(format) || (format == EVO_CACHE_FP32 && head_dim == 128) ? 16 : 32;
 }
 
 }  // namespace
@@ -1196,9 +1236,7 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   AttPlan p = {};
   const int group = n_heads / n_kv_heads;
   const int64_t rows = (int64_t)r.max_rows * group;  // of one sequence and key/value head
-  // (two row blocks of a block of fp32 keys of 128 do not fit the registers)
-  p.tile_rows = rows <= 16 || (format == EVO_CACHE_FP32 && head_dim == 128) ? 16 : 32;
-  if (dtype == EVO_BF16 && rows > 64) p.tile_rows = rows <= 128 ? 128 : 256;
+  p.tile_rows = tile_rows_of(dtype, format, head_dim, rows);
   // row tiles: as many for every sequence, or packed by the rows before
   const int64_t even = (rows + p.tile_rows - 1) / p.tile_rows;
   const int64_t packed = (int64_t)r.n_rows * group / p.tile_rows + r.n_seqs;
@@ -1209,10 +1247,11 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
     p.n_tiles = (int)packed;
   }
   const int64_t blocks = ((int64_t)max_length + kKeys - 1) / kKeys;
-  // parts: two workgroups for every compute unit, each with a block for every wave
   const int64_t wgs = (int64_t)p.n_tiles * n_kv_heads;
+  // parts of the keys: two workgroups for every compute unit (one of eight
+  // waves), each with a few blocks for every wave (see kPartBlocks)
   const int64_t want = wgs ? ((p.tile_rows == 256 ? 1 : 2) * (int64_t)n_cu + wgs - 1) / wgs : 1;
-  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, blocks / kWaves));
+  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, blocks / kPartBlocks));
   if (p.n_split > 1) {
     p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
     p.part_floats = wgs * p.n_split * p.tile_rows * head_dim;

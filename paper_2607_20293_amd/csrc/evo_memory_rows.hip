@@ -214,7 +214,8 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
   constexpr int LPR = DH / 8;  // lanes a row
   const int heads = a.heads_by_rows, groups = a.head_groups;
   const int lane = threadIdx.x % LPR;
-  const int tok = (block / groups) * (kThreads / LPR) + (int)threadIdx.x / LPR, h0 = block % groups;
+  const int at = a.by_groups.divide(block), h0 = block - at * groups;
+  const int tok = at * (kThreads / LPR) + (int)threadIdx.x / LPR;
   // whole waves stay for the exchanges; rows past the end repeat the last one
   // and are not stored
   const bool live = tok < a.rows.n_rows;
@@ -380,10 +381,11 @@ struct ValueRow {
   bool live;
 };
 __device__ __forceinline__ ValueRow value_row(const RowsArgs& a, int block) {
-  const int w = block * (kThreads / 64) + (int)(threadIdx.x >> 6);
+  const int w = __builtin_amdgcn_readfirstlane(block * (kThreads / 64) + (int)(threadIdx.x >> 6));
   ValueRow r;
-  r.h = w % a.n_kv_heads;
-  const int64_t n = (int64_t)(w / a.n_kv_heads) * 64 + (threadIdx.x & 63);
+  const int tile = a.by_kv_heads.divide(w);
+  r.h = w - tile * a.n_kv_heads;
+  const int64_t n = (int64_t)tile * 64 + (threadIdx.x & 63);
   r.live = n < a.rows.n_rows;
   r.n = r.live ? (int)n : a.rows.n_rows - 1;
   int seq, i;
@@ -477,13 +479,14 @@ __device__ __forceinline__ void read_keys(const RowsArgs& a, int block) {
   constexpr int LPR = DH / 8;
   const int ps = a.cache.page_shift, groups = a.head_groups;
   const int lane = threadIdx.x % LPR;
-  const int n = (block / groups) * (kThreads / LPR) + (int)threadIdx.x / LPR;
+  const int at = a.by_groups.divide(block);
+  const int n = at * (kThreads / LPR) + (int)threadIdx.x / LPR;
   if (n >= a.rows.n_rows) return;
   int seq, i;
   find_row(a.rows, n, &seq, &i);
   const int pos = a.starts[seq] + i;
   const int64_t b = block_of(a, seq, pos, 0);
-  for (int h = block % groups; h < a.heads_by_rows; h += groups) {
+  for (int h = block - at * groups; h < a.heads_by_rows; h += groups) {
     const bool is_v = h >= a.n_kv_heads;
     const int hk = is_v ? h - a.n_kv_heads : h;
     float x[8] = {};
@@ -588,6 +591,8 @@ template <int DH> int divide(RowsArgs* a, bool values) {
   const int64_t blocks = ((int64_t)a->rows.n_rows + per - 1) / per;
   a->head_groups = (int)std::max<int64_t>(1, std::min<int64_t>(a->heads_by_rows, (kFill + blocks - 1) / blocks));
   a->qk_blocks = (int)(blocks * a->head_groups);
+  a->by_groups = Divisor::of(a->head_groups);
+  a->by_kv_heads = Divisor::of(std::max(a->n_kv_heads, 1));
   return a->qk_blocks + (by_rows ? 0 : (int)((waves + kThreads / 64 - 1) / (kThreads / 64)));
 }
 
