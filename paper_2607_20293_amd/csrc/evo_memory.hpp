@@ -97,7 +97,7 @@ struct AttArgs {
 };
 
 struct AttPlan {
-  int tile_rows, tiles_per_seq, n_tiles, n_split;
+  int tile_rows, tiles_per_seq, n_tiles, n_split, waves;
   int64_t part_floats, ml_floats;
 };
 

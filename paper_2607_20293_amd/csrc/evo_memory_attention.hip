@@ -418,17 +418,18 @@ template <typename T> __device__ __forceinline__ void store4(T* p, int wide, f32
 
 // Workgroup (row tile, key/value head, part of the keys).
 // Waves that a SIMD shall hold: what the registers of a wave's block allow.
-template <typename T> constexpr int waves_per_simd(int f, int dh, int r) {
+template <typename T> constexpr int waves_per_simd(int f, int dh, int r, int nw) {
+  if (nw == 8) return 2;
   if (sizeof(T) == 4) return dh == 128 || (dh == 64 && r == 2) ? 1 : 2;
   return dh == 128 && f == EVO_CACHE_BF16 ? 1 : r == 2 || dh == 128 ? 2 : 3;
 }
 
-template <typename T, int F, int DH, int R>
-__global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stream_kernel(AttArgs a) {
+template <typename T, int F, int DH, int R, int NW>
+__global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stream_kernel(AttArgs a) {
   typedef Lay<F, DH> L;
   constexpr int TR = 16 * R;
-  __shared__ __attribute__((aligned(16))) float join_o[2][TR * DH];
-  __shared__ float join_ml[kWaves][TR][2];
+  __shared__ __attribute__((aligned(16))) float join_o[NW / 2][TR * DH];
+  __shared__ float join_ml[NW][TR][2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, g = lane >> 4;
   int tile, h, split, seq;
@@ -436,13 +437,13 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
   if (!find_unit(a, blockIdx.x, &tile, &h, &split) || !find_tile(a, tile, TR, &seq, &wh)) return;
   const int th = tile * a.cache.n_kv_heads + h;
   const Blocks bl = blocks_of(a, wh);
-  const int per = max(a.by_split.divide(bl.count + a.n_split - 1), kWaves);
+  const int per = max(a.by_split.divide(bl.count + a.n_split - 1), NW);
   const int v0 = split * per, v1 = min(v0 + per, bl.count);
   const int ps = a.cache.page_shift;
   Sight sight;
   sight.set(a, wh);
   Pages pages;
-  pages.load(a, bl, seq, v0 + w, kWaves);
+  pages.load(a, bl, seq, v0 + w, NW);
 
   // Scores in units of log2 are off + mul x, mul > 0, with x the products by
   //   plain: one factor, inside the exponential (codes: with the key's scale)
@@ -521,11 +522,11 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
     load_keys(bl.at(v) * kKeys, page);
     load_values(bl.at(v) * kKeys, page);
   }
-  for (int it = 1; v < v1; v += kWaves, ++it) {
-    const int kb = bl.at(v) * kKeys, next = v + kWaves < v1 ? bl.at(v + kWaves) * kKeys : -1;
+  for (int it = 1; v < v1; v += NW, ++it) {
+    const int kb = bl.at(v) * kKeys, next = v + NW < v1 ? bl.at(v + NW) * kKeys : -1;
     const int64_t b = (int64_t)page * a.cache.n_kv_heads + h;
     const int slot = kb & ((1 << ps) - 1);
-    if ((it & 63) == 0) pages.load(a, bl, seq, v + kWaves, kWaves);
+    if ((it & 63) == 0) pages.load(a, bl, seq, v + NW, NW);
     page = pages.at(it);
     const bool masked = !sight.all(kb);
     float ks[4][4], vs[4][4];
@@ -629,7 +630,7 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  // ---- the four waves' results, in the order (w0 + w2) + (w1 + w3) ----
+  // ---- the waves' results, in pairs: w and w + NW / 2, then w and w + NW / 4, .. ----
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     l[r] = over_groups(l[r], false);
@@ -643,10 +644,10 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     float M = -kInf;
-    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, join_ml[i][r * 16 + lr][0]);
+    for (int i = 0; i < NW; ++i) M = fmaxf(M, join_ml[i][r * 16 + lr][0]);
     const float base = M == -kInf ? 0.f : M;
     float t = 0.f;
-    for (int i = 0; i < kWaves; ++i) t += join_ml[i][r * 16 + lr][1] * exp2_(join_ml[i][r * 16 + lr][0] - base);
+    for (int i = 0; i < NW; ++i) t += join_ml[i][r * 16 + lr][1] * exp2_(join_ml[i][r * 16 + lr][0] - base);
     total[r] = t;
     top[r] = M;
     const float f = exp2_(m[r] - base);
@@ -665,13 +666,16 @@ __global__ void __launch_bounds__(kWaves * 64, waves_per_simd<T>(F, DH, R)) stre
 #pragma unroll
       for (int c = 0; c < L::CT; ++c) o[r][c] += *reinterpret_cast<const f32x4*>(src + ((r * L::CT + c) * 64 + lane) * 4);
   };
-  if (w >= 2) put(join_o[w - 2]);
+  if (w >= NW / 2) put(join_o[w - NW / 2]);
   __syncthreads();
-  if (w < 2) add(join_o[w]);
-  if (w == 1) put(join_o[1]);  // (the place that it has just read)
-  __syncthreads();
+  if (w < NW / 2) add(join_o[w]);
+#pragma unroll
+  for (int k = NW / 4; k >= 1; k /= 2) {  // waves k .. 2 k - 1 use the place that they have just read
+    if (w >= k && w < 2 * k) put(join_o[w]);
+    __syncthreads();
+    if (w < k) add(join_o[w + k]);
+  }
   if (w != 0) return;
-  add(join_o[1]);
 
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -1189,16 +1193,32 @@ __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
     a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = t == 0.f ? -kInf : (M + __builtin_amdgcn_logf(t)) * kLn2;
 }
 
+// Which formats take two row blocks to a wave, and what leaves a SIMD the
+// registers for two waves (64 int8 chunks of 16 tokens 16.6 us with four waves
+// to a workgroup, 14.3 with eight; 200 fp32 rows, which do not fit, 24 and 32).
+constexpr bool two_row_blocks(int f, int dh) { return !is_coded(f) && !(f == EVO_CACHE_FP32 && dh == 128); }
+constexpr bool eight_waves(int f, int dh, int tile_rows) {
+  return !(tile_rows == 32 && dh * size_of(f) >= 256) && !(f == EVO_CACHE_FP32 && dh == 128);
+}
+
+template <typename T, int F, int DH, int R, int NW>
+void launch_stream(int64_t wgs, const AttArgs& a, hipStream_t stream) {
+  if constexpr (NW == 4 || eight_waves(F, DH, 16 * R))
+    hipLaunchKernelGGL((stream_kernel<T, F, DH, R, NW>), dim3(wgs), dim3(NW * 64), 0, stream, a);
+}
+
 template <typename T, int F, int DH>
 hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
   const int64_t blocks = (int64_t)p.n_tiles * a.cache.n_kv_heads;
   int64_t wgs = blocks * p.n_split;
   if (p.tiles_per_seq > 1) wgs = (wgs / p.tiles_per_seq + 7) / 8 * 8 * p.tiles_per_seq;  // (see find_unit)
+  constexpr int R2 = two_row_blocks(F, DH) ? 2 : 1;
   if (p.tile_rows == 16) {
-    hipLaunchKernelGGL((stream_kernel<T, F, DH, 1>), dim3(wgs), dim3(kWaves * 64), 0, stream, a);
+    if (p.waves == 8) launch_stream<T, F, DH, 1, 8>(wgs, a, stream);
+    else launch_stream<T, F, DH, 1, 4>(wgs, a, stream);
   } else if (p.tile_rows == 32) {
-    if constexpr (!is_coded(F) && !(F == EVO_CACHE_FP32 && DH == 128))
-      hipLaunchKernelGGL((stream_kernel<T, F, DH, 2>), dim3(wgs), dim3(kWaves * 64), 0, stream, a);
+    if (p.waves == 8) launch_stream<T, F, DH, R2, 8>(wgs, a, stream);
+    else launch_stream<T, F, DH, R2, 4>(wgs, a, stream);
   } else if constexpr (sizeof(T) == 2) {
     if (p.tile_rows == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 4>), dim3(wgs), dim3(256), 0, stream, a);
     else if constexpr (DH == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 8>), dim3(wgs), dim3(512), 0, stream, a);
@@ -1226,7 +1246,7 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
 int tile_rows_of(int dtype, int format, int head_dim, int64_t rows) {
   const bool lds = dtype == EVO_BF16 && rows > (is_coded(format) ? 128 : head_dim == 128 ? 32 : 64);
   if (lds) return head_dim == 128 && rows > 128 ? 256 : 128;
-  return rows <= 16 || is_coded(format) || (format == EVO_CACHE_FP32 && head_dim == 128) ? 16 : 32;
+  return rows <= 16 || !two_row_blocks(format, head_dim) ? 16 : 32;
 }
 
 }  // namespace
@@ -1252,6 +1272,8 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   // waves), each with a few blocks for every wave (see kPartBlocks)
   const int64_t want = wgs ? ((p.tile_rows == 256 ? 1 : 2) * (int64_t)n_cu + wgs - 1) / wgs : 1;
   p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, blocks / kPartBlocks));
+  // a workgroup that has its compute unit to itself brings eight waves
+  p.waves = wgs * p.n_split <= n_cu && eight_waves(format, head_dim, p.tile_rows) ? 8 : kWaves;
   if (p.n_split > 1) {
     p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
     p.part_floats = wgs * p.n_split * p.tile_rows * head_dim;
