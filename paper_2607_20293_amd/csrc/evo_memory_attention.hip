@@ -123,6 +123,9 @@ struct Where {
   int row0, rows, base, p_first, p_last, ctx, start, prefix;
 };
 
+// The first row of a sequence, inside the call's rows whatever cu_rows holds.
+__device__ __forceinline__ int first_row(const RowsView& r, int seq) { return min(max(r.cu[seq], 0), r.n_rows); }
+
 // The row tile of a workgroup; false if it has no rows.
 __device__ __forceinline__ bool find_tile(const AttArgs& a, int tile, int tile_rows, int* seq_out, Where* w) {
   int seq, j;
@@ -133,15 +136,15 @@ __device__ __forceinline__ bool find_tile(const AttArgs& a, int tile, int tile_r
     int lo = 0, hi = a.rows.n_seqs;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (a.rows.cu[mid] * a.group / tile_rows + mid <= tile) lo = mid;
+      if (first_row(a.rows, mid) * a.group / tile_rows + mid <= tile) lo = mid;
       else hi = mid;
     }
     seq = lo;
-    j = tile - (a.rows.cu[lo] * a.group / tile_rows + lo);
+    j = tile - (first_row(a.rows, lo) * a.group / tile_rows + lo);
   }
   int r0, n;
   if (a.rows.cu) {
-    r0 = min(max(a.rows.cu[seq], 0), a.rows.n_rows);
+    r0 = first_row(a.rows, seq);
     n = min(min(max(a.rows.cu[seq + 1], r0), a.rows.n_rows) - r0, a.rows.max_rows);
   } else {
     r0 = seq * a.rows.max_rows;

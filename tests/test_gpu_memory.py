@@ -455,3 +455,19 @@ def test_tables_and_lengths_that_lie_outside():
     got = evo.chunk_attention(c.q, cache, i32(c.tab, dev), i32([100, -7], dev), i32([0, 4, 1 << 30], dev), 5, causal=True)
     torch.cuda.synchronize()
     assert torch.equal(got[0][:4], want[0][:4])
+
+
+@pytest.mark.parametrize("rows", [15, 150])
+def test_row_numbers_that_lie_outside(rows):
+    """cu_rows whose entries are any 32-bit numbers: no access leaves the call's
+    rows, and rows that they still name are right."""
+    dev = device()
+    c = Call(dev, "bf16", "bf16", [rows, 4], [170, 90], 4, 2, 64, seed=11, causal=True)
+    want = c.run()
+    cache = evo.KVCache(*c.tensors)
+    n = rows + 4
+    for cu in ([-2 ** 31, rows, n], [0, rows, 2 ** 31 - 1], [0, rows, -2 ** 31], [2 ** 31 - 1, -2 ** 31, n]):
+        got = evo.chunk_attention(c.q, cache, i32(c.tab, dev), i32([170, 90], dev), i32(cu, dev), n, causal=True)
+        torch.cuda.synchronize()
+        if cu[:2] == [0, rows]:
+            assert torch.equal(got[0][:rows], want[0][:rows]), cu
