@@ -45,6 +45,13 @@ constexpr float kInf = __builtin_inff();
 constexpr bool is_coded(int f) { return f == EVO_CACHE_INT8 || f == EVO_CACHE_FP8; }
 constexpr int size_of(int f) { return f == EVO_CACHE_FP32 ? 4 : f == EVO_CACHE_BF16 ? 2 : 1; }
 
+// LDS that one wave writes and reads: its accesses are in order, the compiler
+// has to keep them so
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // maximum / sum over the four lanes lane % 16 of a wave
@@ -197,6 +204,25 @@ __device__ __forceinline__ bool sees(const AttArgs& a, const Where& w, int p, in
   const bool near = (!a.causal || j <= p) && (!a.window || abs(p - j) < a.window);
   return j < w.ctx && (j < w.prefix || near);
 }
+// The same as a run of positions and the prefix, found once for a row: two
+// comparisons a key instead of some ten operations.
+struct Seen {
+  int lo;
+  unsigned span;
+  int prefix;
+  __device__ __forceinline__ Seen(const AttArgs& a, const Where& w, int p) {
+    lo = 0;
+    int hi = w.ctx;
+    if (a.causal) hi = min(hi, p + 1);
+    if (a.window) {
+      hi = min(hi, p + a.window);
+      lo = max(0, p - a.window + 1);
+    }
+    span = (unsigned)max(hi - lo, 0);
+    prefix = w.prefix;
+  }
+  __device__ __forceinline__ bool at(int j) const { return (unsigned)(j - lo) < span || j < prefix; }
+};
 // Which blocks (by their first key) some row of a tile sees, and which all of
 // its rows see whole.
 struct Sight {
@@ -374,6 +400,27 @@ template <int F> __device__ __forceinline__ float not_finite(const void* v, int6
   return (x & 0x7f800000u) == 0x7f800000u ? __builtin_bit_cast(float, x) : 0.f;
 }
 
+// Whether a lane's values hold a NaN or an infinity, in two or three operations
+// a dword: most masked blocks hold none, and then terms of 0 are enough.
+template <int F, int CT, int VW> __device__ __forceinline__ bool any_not_finite(const uint32_t (&v)[CT][VW]) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  uint32_t top = 0;
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int i = 0; i < VW; ++i) {
+      const uint32_t x = v[c][i];
+      if constexpr (F == EVO_CACHE_FP32) top = max(top, x & 0x7fffffffu);
+      if constexpr (F == EVO_CACHE_BF16)
+        top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, x & 0x7fff7fffu)));
+      if constexpr (F == EVO_CACHE_FP8) top |= (x & 0x7f7f7f7fu) + 0x01010101u;
+    }
+  if constexpr (F == EVO_CACHE_FP32) return top >= 0x7f800000u;
+  if constexpr (F == EVO_CACHE_BF16) return top >= 0x7f800000u || (top & 0xffffu) >= 0x7f80u;
+  if constexpr (F == EVO_CACHE_FP8) return top & 0x80808080u;
+  return false;
+}
+
 // A masked block's values: keys past the cache's length become 0 (a page's
 // unused end may hold anything), NaNs and infinities too; returns whether
 // there were any.
@@ -433,6 +480,8 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
   constexpr int TR = 16 * R;
   __shared__ __attribute__((aligned(16))) float join_o[NW / 2][TR * DH];
   __shared__ float join_ml[NW][TR][2];
+  // scales of a wave's block, keys' and values'
+  __shared__ __attribute__((aligned(16))) float scales[is_coded(F) ? NW : 1][2][is_coded(F) ? kKeys : 4];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, g = lane >> 4;
   int tile, h, split, seq;
@@ -469,7 +518,6 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
     pos[r] = wh.start + tok;
     slope[r] = a.slopes ? a.slopes[head] * kLog2e : 0.f;
     load_query<F, DH>(q[r], reinterpret_cast<const T*>(a.q.p) + (wh.row0 + tok) * a.q.row + head * a.q.head, g, a.wide);
-    if (flip) q[r].negate();
   }
   f32x4 o[R][L::CT];
   float m[R], l[R];
@@ -519,11 +567,28 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
       }
   };
 
+  // Scales come a key a lane, a block ahead like the keys, and reach the lanes
+  // that want them through LDS: asked for in that order, 16 a lane, they were
+  // waited for in every block.
+  float k_scale = 0.f, v_scale = 0.f;
+  const auto load_scales = [&](int kb, int page) {
+    if constexpr (is_coded(F)) {
+      const int64_t at = (((int64_t)page * a.cache.n_kv_heads + h) << ps) + (kb & ((1 << ps) - 1)) + lane;
+      k_scale = a.cache.ks[at];
+      v_scale = a.cache.vs[at];
+    }
+  };
+
   int v = v0 + w;
   int page = pages.at(0);
   if (v < v1) {
+    load_scales(bl.at(v) * kKeys, page);
     load_keys(bl.at(v) * kKeys, page);
     load_values(bl.at(v) * kKeys, page);
+  }
+  if (flip) {  // (here: no load waits for the query)
+#pragma unroll
+    for (int r = 0; r < R; ++r) q[r].negate();
   }
   for (int it = 1; v < v1; v += NW, ++it) {
     const int kb = bl.at(v) * kKeys, next = v + NW < v1 ? bl.at(v + NW) * kKeys : -1;
@@ -532,24 +597,23 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
     if ((it & 63) == 0) pages.load(a, bl, seq, v + NW, NW);
     page = pages.at(it);
     const bool masked = !sight.all(kb);
-    float ks[4][4], vs[4][4];
     if constexpr (is_coded(F)) {
-      const int64_t at = (b << ps) + slot;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(a.cache.ks + at + L::key_of(t, g, 0));
-        const f32x4 y = *reinterpret_cast<const f32x4*>(a.cache.vs + at + L::key_of(t, g, 0));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { ks[t][i] = x[i] * pre; vs[t][i] = y[i]; }
-      }
+      wave_sync();
+      scales[w][0][lane] = k_scale * pre;
+      scales[w][1][lane] = v_scale;
+      wave_sync();
     }
+    const auto scale_of = [&](int which, int t) { return *reinterpret_cast<const f32x4*>(&scales[w][which][L::key_of(t, g, 0)]); };
     f32x4 s[R][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int r = 0; r < R; ++r) s[r][t] = score_tile<F, DH>(kr[t], q[r]);
     __builtin_amdgcn_sched_barrier(0);
-    if (next >= 0) load_keys(next, page);
+    if (next >= 0) {
+      load_scales(next, page);
+      load_keys(next, page);
+    }
     __builtin_amdgcn_sched_barrier(0);
 
     Terms<T> terms[R];
@@ -562,7 +626,16 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
 #pragma unroll
           for (int i = 0; i < 4; ++i) f(x[t][i], t, i);
       };
-      each([&](float& x, int t, int i) { x = is_coded(F) ? s[r][t][i] * ks[t][i] : s[r][t][i]; });
+      each([&](float& x, int t, int i) { x = s[r][t][i]; });
+      const auto times = [&](int which) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const f32x4 y = scale_of(which, t);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[t][i] *= y[i];
+        }
+      };
+      if constexpr (is_coded(F)) times(0);
       if (capped) {
         each([&](float& x, int, int) { x = __builtin_amdgcn_rcpf(-1.f - exp2_(is_coded(F) ? x : x * pre)); });
       } else if (!plain) {
@@ -571,7 +644,8 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
         if (a.slopes)
           each([&](float& x, int t, int i) { x = fmaf(-slope[r], fabsf((float)(pos[r] - kb - L::key_of(t, g, i))), x); });
       }
-      if (masked) each([&](float& x, int t, int i) { x = sees(a, wh, pos[r], kb + L::key_of(t, g, i)) ? x : -kInf; });
+      const Seen seen(a, wh, pos[r]);
+      if (masked) each([&](float& x, int t, int i) { x = seen.at(kb + L::key_of(t, g, i)) ? x : -kInf; });
       float top = x[0][0];
       each([&](float& x, int, int) { top = fmaxf(top, x); });
       top = over_groups(fmaf(top, mul, off), true);
@@ -591,13 +665,13 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
       l[r] += sum;
       if constexpr (is_coded(F)) {
         // (an unseen key's scale may be a NaN)
-        if (masked) each([&](float& x, int t, int i) { x = sees(a, wh, pos[r], kb + L::key_of(t, g, i)) ? x * vs[t][i] : 0.f; });
-        else each([&](float& x, int t, int i) { x *= vs[t][i]; });
+        times(1);
+        if (masked) each([&](float& x, int t, int i) { x = seen.at(kb + L::key_of(t, g, i)) ? x : 0.f; });
       }
       terms[r].set(x);
     }
     bool bad = false;
-    if (masked) {
+    if (masked && __any(any_not_finite<F>(vr))) {
       // What a row does not see must not reach it, but 0 times a NaN or an
       // infinity is NaN: those are taken out of the operand, and added below
       // to the rows that see them.
@@ -1061,12 +1135,13 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
             s[t][e] = z;
           }
       }
+      const Seen seen(a, wh, pos);
       if (masked) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (!sees(a, wh, pos, key_at(t, e))) s[t][e] = -kInf;
+            if (!seen.at(key_at(t, e))) s[t][e] = -kInf;
       }
       float top = s[0][0];
 #pragma unroll
@@ -1101,7 +1176,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
           for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (!sees(a, wh, pos, key_at(t, e))) s[t][e] = 0.f;
+              if (!seen.at(key_at(t, e))) s[t][e] = 0.f;
         }
       }
 #pragma unroll
