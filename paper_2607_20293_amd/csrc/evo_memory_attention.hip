@@ -34,10 +34,13 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kKeys = 64;     // keys of a block
 constexpr int kWaves = 4;
-// Least blocks of a part of the keys.  A part costs a second launch to join it:
-// one token over 1000 positions took 15.8, 15.6 and 13.4 us with 4, 8 and 16, 200
-// fp32 rows with a window 34.8, 24.4 and 24.4 us.
-constexpr int kPartBlocks = 16;
+// Least blocks of a part of the keys, for so many workgroups without parts.  A
+// part costs a second launch to join it, which pays where few of the compute
+// units would work: one token over 1000 positions (4 workgroups) takes 8.6, 10.9
+// and 11.7 us with parts of 4, 8 and 16, over 4000 10.1, 11.4 and 16.5; 24 chunks
+// of 16 fp32 rows over 2500 (96) 29.4, 27.0 and 30.8; 32 chunks over 1500 int8
+// positions (128) 11.4, 11.2 and 10.4, 64 (256) 15.6 with 8 and 11.7 with 16.
+constexpr int part_blocks(int64_t wgs, int n_cu) { return 4 * wgs <= n_cu ? 4 : 2 * wgs < n_cu ? 8 : 16; }
 constexpr int kRing = 6;      // operands of a long chunk's products on their way from LDS
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
@@ -1347,11 +1350,12 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   const int64_t blocks = ((int64_t)max_length + kKeys - 1) / kKeys;
   const int64_t wgs = (int64_t)p.n_tiles * n_kv_heads;
   // parts of the keys: two workgroups for every compute unit (one of eight
-  // waves), each with a few blocks for every wave (see kPartBlocks)
+  // waves), each with a few blocks for every wave (part_blocks)
   const int64_t want = wgs ? ((p.tile_rows == 256 ? 1 : 2) * (int64_t)n_cu + wgs - 1) / wgs : 1;
-  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, blocks / kPartBlocks));
-  // a workgroup that has its compute unit to itself brings eight waves
-  p.waves = wgs * p.n_split <= n_cu && eight_waves(format, head_dim, p.tile_rows) ? 8 : kWaves;
+  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, blocks / part_blocks(wgs, n_cu)));
+  // a workgroup that has its compute unit to itself brings eight waves, unless its
+  // part has fewer blocks than that
+  p.waves = wgs * p.n_split <= n_cu && (p.n_split == 1 || blocks / p.n_split >= 8) && eight_waves(format, head_dim, p.tile_rows) ? 8 : kWaves;
   if (p.n_split > 1) {
     p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
     p.part_floats = wgs * p.n_split * p.tile_rows * head_dim;
