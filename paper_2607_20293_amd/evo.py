@@ -640,7 +640,6 @@ class Attention(ctypes.Structure):
 
 CACHE_FP32, CACHE_BF16, CACHE_INT8, CACHE_FP8 = 0, 1, 2, 3
 _PAIRS = {"halves": 0, "adjacent": 1}
-_ref = ctypes.byref
 
 
 def _row_dtype(t) -> int:
@@ -652,7 +651,9 @@ def _row_dtype(t) -> int:
 
 
 # The checks below run at every call of operators that take a few microseconds:
-# one comparison of everything, the reason looked for only where it fails.
+# one comparison of everything, the reason looked for only where it fails;
+# nothing checked of tensors made here; sizes as numbers and structures as they
+# are, which torch and ctypes take faster than tuples and references.
 def _wrong(name, t, dtype, shape, device):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a tensor")
@@ -673,6 +674,12 @@ def _heads(name, t, dtype, shape, device) -> Heads:
     return Heads(t.data_ptr(), row, head)
 
 
+def _new(like, rows, heads, dh):
+    """A contiguous [rows][heads][dh] tensor like another, and its Heads."""
+    t = like.new_empty(rows, heads, dh)
+    return t, Heads(t.data_ptr(), heads * dh, dh)
+
+
 def _ptr(name, t, dtype, shape, device) -> int:
     if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
             or not t.is_contiguous()):
@@ -690,8 +697,11 @@ def _current_stream(index: int) -> int:
     return torch.cuda.current_stream(index).cuda_stream
 
 
-# (the handle alone, without the Stream object around it, where torch has that)
+# (the handle alone, without the Stream object around it, and the device without
+# a look at whether torch has begun, where torch has that: tensors on a device
+# are there already)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _enqueue(device, stream, made, call, *args):
@@ -704,7 +714,7 @@ def _enqueue(device, stream, made, call, *args):
         if handle != _current_stream(device.index):
             for t in made:
                 t.record_stream(stream)
-    if torch.cuda.current_device() == device.index:
+    if _current_device() == device.index:
         rc = call(*args, handle)
     else:
         with torch.cuda.device(device):
@@ -803,17 +813,21 @@ def qk_norm_rope(q, k, positions, table, q_gain=None, k_gain=None, eps: Optional
     dt, dtype = _row_dtype(q), q.dtype
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [rows][heads][dh]")
-    qs = q.shape
-    n, hq, dh = qs
+    n, hq, dh = q.shape
     hk = k.shape[1]
-    ks = (n, hk, dh)
+    qs, ks = (n, hq, dh), (n, hk, dh)
     nr = _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device)
-    made = (q.new_empty(qs), q.new_empty(ks)) if out is None else ()
-    q_out, k_out = made or out
-    _enqueue(device, stream, made, lib().evo_qk_norm_rope, _ref(nr), dt, dh, n, hq, hk,
-             _ref(_heads("q", q, dtype, qs, device)), _ref(_heads("k", k, dtype, ks, device)),
-             None if table is None else _ptr("positions", positions, torch.int32, (n,), device),
-             _ref(_heads("q_out", q_out, dtype, qs, device)), _ref(_heads("k_out", k_out, dtype, ks, device)))
+    made = ()
+    if out is None:
+        q_out, qo = _new(q, n, hq, dh)
+        k_out, ko = _new(q, n, hk, dh)
+        made = (q_out, k_out)
+    else:
+        q_out, k_out = out
+        qo, ko = _heads("q_out", q_out, dtype, qs, device), _heads("k_out", k_out, dtype, ks, device)
+    _enqueue(device, stream, made, lib().evo_qk_norm_rope, nr, dt, dh, n, hq, hk, _heads("q", q, dtype, qs, device),
+             _heads("k", k, dtype, ks, device),
+             None if table is None else _ptr("positions", positions, torch.int32, (n,), device), qo, ko)
     return q_out, k_out
 
 
@@ -823,9 +837,9 @@ def cache_write(cache: KVCache, page_table, starts, k, v, cu_rows=None, max_rows
     device, dtype = cache.device, k.dtype
     dt, shape = _row_dtype(k), (k.shape[0], cache.n_kv_heads, cache.head_dim)
     rows = cache.rows(page_table, shape[0], cu_rows, max_rows)
-    _enqueue(device, stream, (), lib().evo_cache_write, _ref(cache.desc), _ref(rows), dt,
-             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), _ref(_heads("k", k, dtype, shape, device)),
-             _ref(_heads("v", v, dtype, shape, device)))
+    _enqueue(device, stream, (), lib().evo_cache_write, cache.desc, rows, dt,
+             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), _heads("k", k, dtype, shape, device),
+             _heads("v", v, dtype, shape, device))
 
 
 def cache_read(cache: KVCache, page_table, starts, n_rows: int, dtype, cu_rows=None, max_rows: Optional[int] = None,
@@ -834,12 +848,15 @@ def cache_read(cache: KVCache, page_table, starts, n_rows: int, dtype, cu_rows=N
     [n_rows][kv_heads][dh] of dtype."""
     device, shape = cache.device, (n_rows, cache.n_kv_heads, cache.head_dim)
     rows = cache.rows(page_table, n_rows, cu_rows, max_rows)
-    new = cache.k.new_empty
-    made = (new(shape, dtype=dtype), new(shape, dtype=dtype)) if out is None else ()
-    k, v = made or out
-    _enqueue(device, stream, made, lib().evo_cache_read, _ref(cache.desc), _ref(rows), _row_dtype(k),
-             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device),
-             _ref(_heads("k_out", k, dtype, shape, device)), _ref(_heads("v_out", v, dtype, shape, device)))
+    made = ()
+    if out is None:
+        made = k, v = [cache.k.new_empty(*shape, dtype=dtype) for _ in range(2)]
+        ko, vo = [Heads(t.data_ptr(), shape[1] * shape[2], shape[2]) for t in made]
+    else:
+        k, v = out
+        ko, vo = _heads("k_out", k, dtype, shape, device), _heads("v_out", v, dtype, shape, device)
+    _enqueue(device, stream, made, lib().evo_cache_read, cache.desc, rows, _row_dtype(k),
+             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), ko, vo)
     return k, v
 
 
@@ -857,12 +874,15 @@ def qkv_write(cache: KVCache, page_table, starts, q, k, v, table, q_gain=None, k
     qs, ks = (n, hq, dh), (n, cache.n_kv_heads, dh)
     rows = cache.rows(page_table, n, cu_rows, max_rows)
     nr = _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device)
-    made = (q.new_empty(qs),) if q_out is None else ()
-    q_out, = made or (q_out,)
-    _enqueue(device, stream, made, lib().evo_qkv_write, _ref(cache.desc), _ref(rows), _ref(nr), dt, hq,
-             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), _ref(_heads("q", q, dtype, qs, device)),
-             _ref(_heads("k", k, dtype, ks, device)), _ref(_heads("v", v, dtype, ks, device)),
-             _ref(_heads("q_out", q_out, dtype, qs, device)))
+    made = ()
+    if q_out is None:
+        q_out, qo = _new(q, n, hq, dh)
+        made = (q_out,)
+    else:
+        qo = _heads("q_out", q_out, dtype, qs, device)
+    _enqueue(device, stream, made, lib().evo_qkv_write, cache.desc, rows, nr, dt, hq,
+             _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), _heads("q", q, dtype, qs, device),
+             _heads("k", k, dtype, ks, device), _heads("v", v, dtype, ks, device), qo)
     return q_out
 
 
@@ -876,7 +896,7 @@ def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_ro
     plan alone (0: the page table's).  Returns (out [rows][heads][dh], lse
     float32 [rows][heads])."""
     device, dh, dtype = cache.device, cache.head_dim, q.dtype
-    if torch.cuda.current_device() != device.index:  # (the plan is the current device's)
+    if _current_device() != device.index:  # (the plan is the current device's)
         with torch.cuda.device(device):
             return chunk_attention(q, cache, page_table, lengths, cu_rows, max_rows, scale=scale, causal=causal,
                                    window=window, cap=cap, slopes=slopes, prefix=prefix, starts=starts,
@@ -896,19 +916,23 @@ def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_ro
     L, desc = lib(), cache.desc
     made = []
     if out is None:
-        out = q.new_empty(qs)
+        out, ho = _new(q, n, hq, dh)
         made.append(out)
+    else:
+        ho = _heads("out", out, dtype, qs, device)
     if lse is None:
-        lse = q.new_empty((n, hq), dtype=torch.float32)
+        lse = q.new_empty(n, hq, dtype=torch.float32)
+        lse_at = lse.data_ptr()
         made.append(lse)
-    hs, ho = _heads("q", q, dtype, qs, device), _heads("out", out, dtype, qs, device)
-    need = L.evo_chunk_attention_workspace(_ref(desc), _ref(rows), _ref(att))
+    else:
+        lse_at = _ptr("lse", lse, torch.float32, (n, hq), device)
+    need = L.evo_chunk_attention_workspace(desc, rows, att)
     work = None
     if need:
         if need < 0:
             _check(int(need))
-        made.append(q.new_empty((need,), dtype=torch.uint8))
+        made.append(q.new_empty(need, dtype=torch.uint8))
         work = made[-1].data_ptr()
-    _enqueue(device, stream, made, L.evo_chunk_attention, _ref(desc), _ref(rows), _ref(att), _ref(hs), _ref(ho),
-             _ptr("lse", lse, torch.float32, (n, hq), device), work, need)
+    _enqueue(device, stream, made, L.evo_chunk_attention, desc, rows, att, _heads("q", q, dtype, qs, device), ho, lse_at,
+             work, need)
     return out, lse
