@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <chrono>
 #include <cmath>
 
 #include "evo_host.hpp"
@@ -179,7 +180,19 @@ AttPlan plan_of(const evo_kv_cache* c, const RowsView& r, const evo_attention* t
   return plan_attention(t->dtype, c->format, c->head_dim, t->n_heads, c->n_kv_heads, r, (int)length, t->window,
                         t->causal != 0, compute_units());
 }
-int64_t bytes_of(const AttPlan& p) { return (p.part_floats + p.ml_floats) * (int64_t)sizeof(float); }
+int64_t bytes_of(const AttPlan& p) {
+  return (p.part_floats + p.ml_floats) * (int64_t)sizeof(float) + p.flags * (int64_t)sizeof(unsigned long long);
+}
+
+// A number that no other call of this process has, and that memory which holds
+// anything is not likely to hold (steps of an odd constant over 64 bits, from
+// the clock; 0 is what cleared flags hold).
+unsigned long long call_number() {
+  static std::atomic<unsigned long long> next{
+      (unsigned long long)std::chrono::high_resolution_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull};
+  const unsigned long long n = next.fetch_add(0x9e3779b97f4a7c15ull, std::memory_order_relaxed);
+  return n ? n : call_number();
+}
 
 }  // namespace
 }  // namespace evo
@@ -346,6 +359,10 @@ int evo_chunk_attention(const evo_kv_cache* cache, const evo_kv_rows* rows, cons
   a.by_split = Divisor::of(p.n_split);
   a.part = (float*)workspace;
   a.part_ml = (float*)workspace + p.part_floats;
+  if (p.flags) {
+    a.flags = (unsigned long long*)(a.part_ml + p.ml_floats);
+    a.number = call_number();
+  }
   return launched(launch_attention(att->dtype, cache->format, cache->head_dim, p, a, (hipStream_t)hip_stream));
 }
 

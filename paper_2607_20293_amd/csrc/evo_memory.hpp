@@ -94,11 +94,13 @@ struct AttArgs {
   Divisor by_group, by_kv_heads, by_tiles, by_eight, by_split;  // (by_eight: 8 sequences' tiles)
   float* part;                // [n_tiles][n_kv_heads][n_split][tile rows][head_dim] unnormalised outputs
   float* part_ml;             // [n_tiles][n_kv_heads][n_split][tile rows][2]: maximum (log2), sum
+  unsigned long long* flags;  // [n_tiles][n_kv_heads][n_split]: `number` where a part is written
+  unsigned long long number;  // of this call
 };
 
 struct AttPlan {
   int tile_rows, tiles_per_seq, n_tiles, n_split, waves;
-  int64_t part_floats, ml_floats;
+  int64_t part_floats, ml_floats, flags;
 };
 
 AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_kv_heads, const RowsView& r,

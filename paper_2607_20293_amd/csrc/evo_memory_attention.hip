@@ -469,6 +469,91 @@ template <typename T> __device__ __forceinline__ void store4(T* p, int wide, f32
   }
 }
 
+// Parts that another workgroup of the launch reads: loads and stores that go
+// past a die's cache (cache policy bit SC1), each die having its own.  Cheaper
+// by far than ordinary ones between fences, which write back and empty the
+// whole cache: 16 chunks of 16 tokens over 2500 fp8 positions took 51 us so.
+constexpr int kCoherent = 16;
+struct Parts {
+  __amdgpu_buffer_rsrc_t o;  // [n_split][tile_rows][head_dim] of one tile and key/value head
+  unsigned long long* ml;
+  template <int DH> __device__ __forceinline__ static Parts of(const AttArgs& a, int th, int tile_rows) {
+    const int64_t first = (int64_t)th * a.n_split * tile_rows;
+    return Parts{__builtin_amdgcn_make_buffer_rsrc(a.part + first * DH, (short)0, a.n_split * tile_rows * DH * 4, 0x00020000),
+                 reinterpret_cast<unsigned long long*>(a.part_ml + first * 2)};
+  }
+};
+// The wave's stores so far have landed, and nothing after this has begun.
+__device__ __forceinline__ void stores_landed() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  asm volatile("" ::: "memory");
+}
+
+// Joins the parts of four channels of a row, in order; eight parts are
+// requested at a time, since a part's load is all latency.
+template <typename T, int DH>
+__device__ __forceinline__ void join_parts(const AttArgs& a, const Where& wh, int th, int h, int tile_rows, int r, int c) {
+  constexpr int AT = 8;
+  const int row = wh.base + r;
+  const Parts parts = Parts::of<DH>(a, th, tile_rows);
+  float M = -kInf, t = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < a.n_split; s0 += AT) {
+    float m[AT], l[AT];
+    f32x4 v[AT];
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const int at = min(s0 + i, a.n_split - 1) * tile_rows + r;
+      const unsigned long long ml = __hip_atomic_load(parts.ml + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      m[i] = __builtin_bit_cast(float, (uint32_t)ml);
+      l[i] = s0 + i < a.n_split ? __builtin_bit_cast(float, (uint32_t)(ml >> 32)) : 0.f;
+      v[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(parts.o, (at * DH + c) * 4, 0, kCoherent));
+    }
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < AT; ++i) top = fmaxf(top, m[i]);
+    const float base = top == -kInf ? 0.f : top, keep = exp2_(M - base);
+    M = top;
+    t *= keep;
+    o *= keep;
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const float f = exp2_(m[i] - base);
+      if (l[i] == 0.f) continue;  // (a part that saw nothing wrote no outputs)
+      t += l[i] * f;
+      o += v[i] * f;
+    }
+  }
+  const int tok = a.by_group.divide(row), head = h * a.group + row - tok * a.group;
+  T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
+  store4(dst + c, a.wide, t == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / t));
+  if (a.lse && c == 0)
+    a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = t == 0.f ? -kInf : (M + __builtin_amdgcn_logf(t)) * kLn2;
+}
+
+// Whether all parts of a row tile are written, asked by the wave that has
+// written its own.  A part's flag is set to the call's number, which no other
+// call of the process has, so that flags need no clearing before; whoever finds
+// all set clears them, for a call that is recorded once and replayed.  A flag is
+// set once the part has landed, and the others are read once the flag has: the
+// writer of the flag that lands last finds all.  Should another find them all
+// too, both join the same parts to the same results.  Nobody waits.
+__device__ __forceinline__ bool parts_complete(const AttArgs& a, int th, int split) {
+  const int lane = threadIdx.x & 63;
+  unsigned long long* flags = a.flags + (int64_t)th * a.n_split;
+  stores_landed();
+  if (lane == 0) __hip_atomic_store(flags + split, a.number, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  stores_landed();
+  bool all = true;
+  for (int i = lane; i < a.n_split; i += 64)
+    all &= __hip_atomic_load(flags + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.number;
+  if (!__all(all)) return false;
+  for (int i = lane; i < a.n_split; i += 64)
+    __hip_atomic_store(flags + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
 // Workgroup (row tile, key/value head, part of the keys).
 // Waves that a SIMD shall hold: what the registers of a wave's block allow.
 template <typename T> constexpr int waves_per_simd(int f, int dh, int r, int nw) {
@@ -477,7 +562,10 @@ template <typename T> constexpr int waves_per_simd(int f, int dh, int r, int nw)
   return dh == 128 && f == EVO_CACHE_BF16 ? 1 : r == 2 || dh == 128 ? 2 : 3;
 }
 
-template <typename T, int F, int DH, int R, int NW>
+// PARTS: the keys are split over workgroups (of its own, because the join's
+// code costs the others registers: 32-token chunks over fp8 memories 47 us with
+// it and 45 without).
+template <typename T, int F, int DH, int R, int NW, bool PARTS>
 __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stream_kernel(AttArgs a) {
   typedef Lay<F, DH> L;
   constexpr int TR = 16 * R;
@@ -492,8 +580,8 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
   if (!find_unit(a, blockIdx.x, &tile, &h, &split) || !find_tile(a, tile, TR, &seq, &wh)) return;
   const int th = tile * a.cache.n_kv_heads + h;
   const Blocks bl = blocks_of(a, wh);
-  const int per = max(a.by_split.divide(bl.count + a.n_split - 1), NW);
-  const int v0 = split * per, v1 = min(v0 + per, bl.count);
+  const int per = PARTS ? max(a.by_split.divide(bl.count + a.n_split - 1), NW) : bl.count;
+  const int v0 = PARTS ? split * per : 0, v1 = PARTS ? min(v0 + per, bl.count) : bl.count;
   const int ps = a.cache.page_shift;
   Sight sight;
   sight.set(a, wh);
@@ -755,24 +843,40 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
     __syncthreads();
     if (w < k) add(join_o[w + k]);
   }
+
+  if constexpr (PARTS) {
+    const Parts parts = Parts::of<DH>(a, th, TR);
+    if (w == 0) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (wh.base + r * 16 + lr >= wh.rows) continue;
+        const int part = split * TR + r * 16 + lr;
+        if (g == 0)
+          __hip_atomic_store(parts.ml + part, __builtin_bit_cast(uint32_t, top[r]) | (unsigned long long)__builtin_bit_cast(uint32_t, total[r]) << 32,
+                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (v0 < v1) {
+          // (the whole offset in a vector register: with a scalar part the wait
+          // states before the data's next change are left out)
+#pragma unroll
+          for (int c = 0; c < L::CT; ++c)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o[r][c]), parts.o, (part * DH + c * 16 + g * 4) * 4, 0, kCoherent);
+        }
+      }
+      const bool complete = parts_complete(a, th, split);
+      if (lane == 0) join_ml[0][0][0] = complete ? 1.f : 0.f;
+    }
+    __syncthreads();
+    if (join_ml[0][0][0] == 0.f) return;
+    for (int x = threadIdx.x; x < min(TR, wh.rows - wh.base) * (DH / 4); x += NW * 64)
+      join_parts<T, DH>(a, wh, th, h, TR, x / (DH / 4), x % (DH / 4) * 4);
+    return;
+  }
   if (w != 0) return;
 
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = wh.base + r * 16 + lr;
     if (row >= wh.rows) continue;
-    if (a.n_split > 1) {
-      const int64_t part = ((int64_t)th * a.n_split + split) * TR + r * 16 + lr;
-      if (g == 0) {
-        a.part_ml[part * 2] = top[r];
-        a.part_ml[part * 2 + 1] = total[r];
-      }
-      if (v0 < v1) {
-#pragma unroll
-        for (int c = 0; c < L::CT; ++c) *reinterpret_cast<f32x4*>(a.part + part * DH + c * 16 + g * 4) = o[r][c];
-      }
-      continue;
-    }
     const int tok = a.by_group.divide(row), head = h * a.group + row - tok * a.group;
     const float inv = total[r] == 0.f ? 0.f : 1.f / total[r];
     T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
@@ -1138,8 +1242,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
             s[t][e] = z;
           }
       }
-      const Seen seen(a, wh, pos);
       if (masked) {
+        const Seen seen(a, wh, pos);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -1175,6 +1279,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
       if constexpr (is_coded(F)) {
         times(scales[i & 1] + 64);
         if (masked) {
+          const Seen seen(a, wh, pos);
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -1226,52 +1331,17 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
     a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Joins the parts of a row tile, in order, a thread four channels of a row;
-// eight parts are requested at a time, since a part's load is all latency.
+// Joins a launch's parts, a thread four channels of a row.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
-  constexpr int AT = 8;
-  const int x = (blockIdx.x * 256 + threadIdx.x) % (tile_rows * (DH / 4));
-  const int th = (blockIdx.x * 256 + threadIdx.x) / (tile_rows * (DH / 4));
+  const int wgs = tile_rows * (DH / 4) / 256;  // of a tile: tile_rows is 128 or 256
+  const int th = blockIdx.x / wgs, x = (blockIdx.x - th * wgs) * 256 + threadIdx.x;
   const int tile = a.by_kv_heads.divide(th), h = th - tile * a.cache.n_kv_heads;
   int seq;
   Where wh;
   if (tile >= a.n_tiles || !find_tile(a, tile, tile_rows, &seq, &wh)) return;
-  const int r = x / (DH / 4), c = x % (DH / 4) * 4, row = wh.base + r;
-  if (row >= wh.rows) return;
-  const int64_t part = (int64_t)th * a.n_split * tile_rows + r;
-  float M = -kInf, t = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < a.n_split; s0 += AT) {
-    float m[AT], l[AT];
-    f32x4 v[AT];
-#pragma unroll
-    for (int i = 0; i < AT; ++i) {
-      const int64_t at = part + (int64_t)min(s0 + i, a.n_split - 1) * tile_rows;
-      m[i] = a.part_ml[at * 2];
-      l[i] = s0 + i < a.n_split ? a.part_ml[at * 2 + 1] : 0.f;
-      v[i] = *reinterpret_cast<const f32x4*>(a.part + at * DH + c);
-    }
-    float top = M;
-#pragma unroll
-    for (int i = 0; i < AT; ++i) top = fmaxf(top, m[i]);
-    const float base = top == -kInf ? 0.f : top, keep = exp2_(M - base);
-    M = top;
-    t *= keep;
-    o *= keep;
-#pragma unroll
-    for (int i = 0; i < AT; ++i) {
-      const float f = exp2_(m[i] - base);
-      if (l[i] == 0.f) continue;  // (a part that saw nothing wrote no outputs)
-      t += l[i] * f;
-      o += v[i] * f;
-    }
-  }
-  const int tok = a.by_group.divide(row), head = h * a.group + row - tok * a.group;
-  T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
-  store4(dst + c, a.wide, t == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / t));
-  if (a.lse && c == 0)
-    a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = t == 0.f ? -kInf : (M + __builtin_amdgcn_logf(t)) * kLn2;
+  const int r = x / (DH / 4);
+  if (wh.base + r < wh.rows) join_parts<T, DH>(a, wh, th, h, tile_rows, r, x % (DH / 4) * 4);
 }
 
 // Which formats take two row blocks to a wave, and what leaves a SIMD the
@@ -1285,7 +1355,8 @@ constexpr bool eight_waves(int f, int dh, int tile_rows) {
 template <typename T, int F, int DH, int R, int NW>
 void launch_stream(int64_t wgs, const AttArgs& a, hipStream_t stream) {
   if constexpr (NW == 4 || eight_waves(F, DH, 16 * R))
-    hipLaunchKernelGGL((stream_kernel<T, F, DH, R, NW>), dim3(wgs), dim3(NW * 64), 0, stream, a);
+    hipLaunchKernelGGL((a.n_split > 1 ? stream_kernel<T, F, DH, R, NW, true> : stream_kernel<T, F, DH, R, NW, false>),
+                       dim3(wgs), dim3(NW * 64), 0, stream, a);
 }
 
 template <typename T, int F, int DH>
@@ -1305,8 +1376,8 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
     else if constexpr (DH == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 8>), dim3(wgs), dim3(512), 0, stream, a);
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.n_split == 1) return e;
-  hipLaunchKernelGGL((join_kernel<T, DH>), dim3((blocks * p.tile_rows * (DH / 4) + 255) / 256), dim3(256), 0, stream, a,
+  if (e != hipSuccess || p.n_split == 1 || p.flags) return e;
+  hipLaunchKernelGGL((join_kernel<T, DH>), dim3(blocks * (p.tile_rows * (DH / 4) / 256)), dim3(256), 0, stream, a,
                      p.tile_rows);
   return hipGetLastError();
 }
@@ -1359,6 +1430,9 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   if (p.n_split > 1) {
     p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
     p.part_floats = wgs * p.n_split * p.tile_rows * head_dim;
+    // few rows are joined by the workgroup that ends last, which saves a launch;
+    // long chunks' tiles by a launch of its own, over all compute units
+    if (p.tile_rows <= 32) p.flags = wgs * p.n_split;
   }
   return p;
 }

@@ -471,3 +471,37 @@ def test_row_numbers_that_lie_outside(rows):
         torch.cuda.synchronize()
         if cu[:2] == [0, rows]:
             assert torch.equal(got[0][:rows], want[0][:rows]), cu
+
+
+@pytest.mark.parametrize("rows,lengths,heads", [([1], [9000], 4), ([16] * 24, [2500] * 24, 4), ([1] * 6, [20000] * 6, 8)])
+def test_joined_parts_at_every_call(rows, lengths, heads):
+    """Parts of the keys that workgroups of one launch join: the same bits at
+    each of many calls, alone and recorded, in memory that other work used."""
+    dev = device()
+    c = Call(dev, "bf16", "bf16", rows, lengths, heads, 4, 64, seed=12, causal=True)
+    cache, tab, lens, cu = evo.KVCache(*c.tensors), i32(c.tab, dev), i32(c.lengths, dev), i32(c.cu, dev)
+
+    def call():
+        return evo.chunk_attention(c.q, cache, tab, lens, cu, max(rows), causal=True)
+    one = evo.chunk_attention(c.q, cache, tab, lens, cu, max(rows), causal=True, max_length=1)    # not in parts
+    want = [t.clone() for t in call()]
+    top = float(c.tensors[1].float().abs().max())
+    assert float((want[0].float() - one[0].float()).abs().max()) <= 2.2 * EPS16 * top
+    side = torch.cuda.Stream(dev)
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        held = call()
+    wrong = torch.zeros((), dtype=torch.int64, device=dev)
+    for r in range(200):
+        got = call()
+        wrong += (got[0] != want[0]).sum() + (got[1] != want[1]).sum()
+        del got
+        if r % 3 == 0:
+            torch.empty(1 << (14 + r % 8), device=dev).normal_()
+        held[0].zero_()
+        graph.replay()
+        wrong += (held[0] != want[0]).sum() + (held[1] != want[1]).sum()
+    assert int(wrong) == 0
