@@ -338,17 +338,12 @@ __device__ __forceinline__ void qk_rows(const RowsArgs& a, int block) {
   }
 }
 
-// A wave's 64 rows of values pass through LDS a slice of BYTES at a time,
+// A wave's 64 rows of values pass through LDS a slice of kSlice bytes at a time,
 // because a lane that reads (or writes) a row of its own touches a cache line 16
 // bytes at a time: staged, P lanes take a row's part of a slice, RP rows at once.
-// Slices of whole lines for rows of 256 bytes and more (8 memories of 128 in fp8
-// written and read 150 us, halves 154; two in bf16 119 and 125); of half a line
-// for shorter ones, which leaves LDS for twice the waves (int8 rows of 64, 47.5
-// us and 45.3).
+constexpr int kSlice = 128, kPitch = kSlice + 16;
 template <typename T, int DH> struct Slices {
-  static constexpr int BYTES = DH * (int)sizeof(T) >= 256 ? 128 : 64;
-  static constexpr int PITCH = BYTES + 16;
-  static constexpr int N = BYTES / (int)sizeof(T);
+  static constexpr int N = kSlice / (int)sizeof(T);
   static constexpr int V = N < DH ? N : DH;            // values of a row in a slice
   static constexpr int P = V * (int)sizeof(T) / 16;
   static constexpr int RP = 64 / P;
@@ -416,11 +411,11 @@ __device__ __forceinline__ void v_rows(const RowsArgs& a, int block, char* lds, 
 #pragma unroll
     for (int c = 0; c < S::C; ++c) {
       if (a.wide) {
-        w[c][i] = *reinterpret_cast<const u32x4*>(p + c * S::BYTES);
+        w[c][i] = *reinterpret_cast<const u32x4*>(p + c * kSlice);
       } else {
         T* d = reinterpret_cast<T*>(&w[c][i]);
 #pragma unroll
-        for (int e = 0; e < 16 / (int)sizeof(T); ++e) d[e] = reinterpret_cast<const T*>(p + c * S::BYTES)[e];
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) d[e] = reinterpret_cast<const T*>(p + c * kSlice)[e];
       }
     }
   }
@@ -445,13 +440,13 @@ __device__ __forceinline__ void v_rows(const RowsArgs& a, int block, char* lds, 
     wave_sync();
 #pragma unroll
     for (int i = 0; i < S::P; ++i)
-      *reinterpret_cast<u32x4*>(lds + (i * S::RP + lane / S::P) * S::PITCH + (lane % S::P) * 16) = w[c][i];
+      *reinterpret_cast<u32x4*>(lds + (i * S::RP + lane / S::P) * kPitch + (lane % S::P) * 16) = w[c][i];
     wave_sync();
     if (live) {
 #pragma unroll
       for (int j = 0; j < S::V; j += 8) {
         float x[8];
-        load8(reinterpret_cast<const T*>(lds + lane * S::PITCH) + j, 1, x);
+        load8(reinterpret_cast<const T*>(lds + lane * kPitch) + j, 1, x);
         if constexpr (is_coded(F)) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = quotient<F>(x[e], cd);
@@ -470,13 +465,11 @@ __device__ __forceinline__ void v_rows(const RowsArgs& a, int block, char* lds, 
 
 template <typename T, int F, int DH>
 __global__ void __launch_bounds__(kThreads) rows_kernel(RowsArgs a) {
-  __shared__ __attribute__((aligned(16))) char stage[F == kNone ? 1 : kThreads / 64][F == kNone ? 16 : 64 * Slices<T, DH>::PITCH];
+  __shared__ __attribute__((aligned(16))) char stage[F == kNone ? 1 : kThreads / 64][F == kNone ? 16 : 64 * kPitch];
   __shared__ uint32_t tops[F == kNone ? 1 : kThreads];
   const int w = threadIdx.x >> 6;
-  // values first: their waves take longest (8 memories in fp8 150 us, last 158)
-  const int nv = (int)gridDim.x - a.qk_blocks;
-  if ((int)blockIdx.x >= nv) qk_rows<T, F, DH>(a, blockIdx.x - nv);
-  else if constexpr (F != kNone) v_rows<T, F, DH>(a, blockIdx.x, stage[w], tops + w * 64);
+  if ((int)blockIdx.x < a.qk_blocks) qk_rows<T, F, DH>(a, blockIdx.x);
+  else if constexpr (F != kNone) v_rows<T, F, DH>(a, blockIdx.x - a.qk_blocks, stage[w], tops + w * 64);
 }
 
 // ---- reading back: keys a group of lanes a token, values a lane a row ------
@@ -559,14 +552,14 @@ __device__ __forceinline__ void read_values(const RowsArgs& a, int block, char* 
           for (int e = 0; e < 8; ++e) x[e] = (float)p[(int64_t)e << ps];
         }
       }
-      store8(reinterpret_cast<T*>(lds + lane * S::PITCH) + j, 1, x);
+      store8(reinterpret_cast<T*>(lds + lane * kPitch) + j, 1, x);
     }
     wave_sync();
 #pragma unroll
     for (int i = 0; i < S::P; ++i) {
       const int row = i * S::RP + lane / S::P;
-      const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * S::PITCH + (lane % S::P) * 16);
-      char* p = address_of(dst, row) + c * S::BYTES + (lane % S::P) * 16;
+      const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * kPitch + (lane % S::P) * 16);
+      char* p = address_of(dst, row) + c * kSlice + (lane % S::P) * 16;
       if (!(rows >> row & 1)) continue;
       if (a.wide) {
         *reinterpret_cast<u32x4*>(p) = w;
@@ -581,10 +574,9 @@ __device__ __forceinline__ void read_values(const RowsArgs& a, int block, char* 
 
 template <typename T, int F, int DH>
 __global__ void __launch_bounds__(kThreads) read_kernel(RowsArgs a) {
-  __shared__ __attribute__((aligned(16))) char stage[kThreads / 64][64 * Slices<T, DH>::PITCH];
-  const int nv = (int)gridDim.x - a.qk_blocks;
-  if ((int)blockIdx.x >= nv) read_keys<T, F, DH>(a, blockIdx.x - nv);
-  else read_values<T, F, DH>(a, blockIdx.x, stage[threadIdx.x >> 6]);
+  __shared__ __attribute__((aligned(16))) char stage[kThreads / 64][64 * kPitch];
+  if ((int)blockIdx.x < a.qk_blocks) read_keys<T, F, DH>(a, blockIdx.x);
+  else read_values<T, F, DH>(a, blockIdx.x - a.qk_blocks, stage[threadIdx.x >> 6]);
 }
 
 // How a launch is divided.  Values go the way of keys, a group of lanes a row,
