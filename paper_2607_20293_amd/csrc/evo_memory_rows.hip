@@ -575,8 +575,11 @@ __device__ __forceinline__ void read_values(const RowsArgs& a, int block, char* 
 template <typename T, int F, int DH>
 __global__ void __launch_bounds__(kThreads) read_kernel(RowsArgs a) {
   __shared__ __attribute__((aligned(16))) char stage[kThreads / 64][64 * kPitch];
-  if ((int)blockIdx.x < a.qk_blocks) read_keys<T, F, DH>(a, blockIdx.x);
-  else read_values<T, F, DH>(a, blockIdx.x - a.qk_blocks, stage[threadIdx.x >> 6]);
+  // values first: what a write left last is read first, from the caches (two
+  // bf16 memories written and read back 120 us, else 124; 8 in fp8 161 and 164)
+  const int nv = (int)gridDim.x - a.qk_blocks;
+  if ((int)blockIdx.x >= nv) read_keys<T, F, DH>(a, blockIdx.x - nv);
+  else read_values<T, F, DH>(a, blockIdx.x, stage[threadIdx.x >> 6]);
 }
 
 // How a launch is divided.  Values go the way of keys, a group of lanes a row,
