@@ -1345,11 +1345,21 @@ __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
 }
 
 // Which formats take two row blocks to a wave, and what leaves a SIMD the
-// registers for two waves (64 int8 chunks of 16 tokens 16.6 us with four waves
-// to a workgroup, 14.3 with eight; 200 fp32 rows, which do not fit, 24 and 32).
+// registers for two waves (200 fp32 rows, which do not fit, 24 us with four waves
+// to a workgroup and 32 with eight).
 constexpr bool two_row_blocks(int f, int dh) { return !is_coded(f) && !(f == EVO_CACHE_FP32 && dh == 128); }
 constexpr bool eight_waves(int f, int dh, int tile_rows) {
   return !(tile_rows == 32 && dh * size_of(f) >= 256) && !(f == EVO_CACHE_FP32 && dh == 128);
+}
+
+// Rows of a sequence and key/value head from which keys and values go through
+// LDS (measured at tile_rows_of).
+constexpr int64_t kNever = 1ll << 40;
+constexpr int64_t lds_rows(int f, int dh) {
+  if (f == EVO_CACHE_FP32) return kNever;
+  if (dh == 128) return f == EVO_CACHE_BF16 ? 33 : 97;
+  if (f == EVO_CACHE_BF16) return dh == 64 ? 65 : 1025;
+  return f == EVO_CACHE_INT8 && dh == 64 ? 2049 : kNever;
 }
 
 template <typename T, int F, int DH, int R, int NW>
@@ -1371,7 +1381,7 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
   } else if (p.tile_rows == 32) {
     if (p.waves == 8) launch_stream<T, F, DH, R2, 8>(wgs, a, stream);
     else launch_stream<T, F, DH, R2, 4>(wgs, a, stream);
-  } else if constexpr (sizeof(T) == 2) {
+  } else if constexpr (sizeof(T) == 2 && lds_rows(F, DH) != kNever) {
     if (p.tile_rows == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 4>), dim3(wgs), dim3(256), 0, stream, a);
     else if constexpr (DH == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 8>), dim3(wgs), dim3(512), 0, stream, a);
   }
@@ -1383,21 +1393,26 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
 }
 
 // Rows of a tile, by the rows that a sequence has for a key/value head.
-// Measured, us of a call (12 heads of 64 over 4000 positions of 16 sequences, or 8
-// heads of 128, grouped by four, over 8000):
-//  * 8-bit caches take 16 rows to a wave up to 128: the registers then hold
-//    three waves to a SIMD, which hide the conversions.  32 rows 34 (two row
-//    blocks to a wave 39), 64 rows 52 (63; through LDS 87), 100 rows 73 (LDS
-//    92); 200 rows of 8 sequences 70 and 73.
-//  * others take two row blocks, which halves the reads: 32 rows 35 (one 47), 64
-//    rows 57 (one 85, LDS 64); heads of 128: 32 rows 89 (129, LDS 95), 64 rows
-//    130 (181, LDS 81).  Two row blocks of fp32 keys of 128 do not fit.
+// Measured, us of a call:
+//  * 8-bit caches take 16 rows to a wave: the registers then hold three waves to
+//    a SIMD, which hide the conversions (two row blocks to a wave: 32-token
+//    chunks over fp8 memories 51, one 45).
+//  * others take two row blocks, which halves the reads (12 heads of 64 over 4000
+//    bf16 positions of 16 sequences: 64 rows 72, one block 88; 32 rows 51 and 50;
+//    32 rows of 128, grouped by four over 8000, 109 and 137; fp32, 64 rows 158
+//    and 201).  Two row blocks of fp32 keys of 128 do not fit.
+//  * LDS pays from lds_rows() on, where a sequence's rows share enough: heads of
+//    128, bf16: 32 rows 109, LDS 113, 64 rows 140 and 119; 8-bit: 96 rows 78 and
+//    91, 128 rows 96 and 76.  Heads of 64, bf16: 64 rows 45 and 46, 80 rows 50 and
+//    46 (2000 positions); int8: 800 rows 250 and 278, 2000 rows of 8 sequences 307
+//    and 280, causal 181 and 208, 4096 rows of one over 12288 586 and 461; fp8 448
+//    and 472 there.  Heads of 32, bf16: 800 rows 96 and 101, 2000 rows 116 and 102,
+//    causal 81 and 85; int8 over 8000 270 and 347.
 //  * through LDS, heads of 128 take tiles of 256 (4096 rows behind 8192 659,
-//    tiles of 128 746; 64 rows, 256 to a head, 76 and 85), the others of 128
-//    (1024 rows behind 1024, 4 sequences, 51, tiles of 256 59; int8 75 and 93).
+//    tiles of 128 746; 64 rows, 256 to a head, 57 and 64), the others of 128
+//    (1024 rows behind 1024, 4 sequences, 51, tiles of 256 59).
 int tile_rows_of(int dtype, int format, int head_dim, int64_t rows) {
-  const bool lds = dtype == EVO_BF16 && rows > (is_coded(format) ? 128 : head_dim == 128 ? 32 : 64);
-  if (lds) return head_dim == 128 && rows > 128 ? 256 : 128;
+  if (dtype == EVO_BF16 && rows >= lds_rows(format, head_dim)) return head_dim == 128 && rows > 128 ? 256 : 128;
   return rows <= 16 || !two_row_blocks(format, head_dim) ? 16 : 32;
 }
 

@@ -505,3 +505,37 @@ def test_joined_parts_at_every_call(rows, lengths, heads):
         graph.replay()
         wrong += (held[0] != want[0]).sum() + (held[1] != want[1]).sum()
     assert int(wrong) == 0
+
+
+@pytest.mark.parametrize("dtype,fmt,rows,lengths,dh,kw", [
+    ("bf16", "int8", [2060, 3], [2100, 700], 64, dict(causal=True, window=900)),
+    ("bf16", "bf16", [1030, 2], [1100, 65], 32, dict(causal=True)),
+    ("bf16", "int8", [100, 97], [300, 130], 128, dict(causal=True, cap=20.0)),
+    ("bf16", "fp8", [130, 20], [190, 500], 128, dict(causal=True, prefix=[170, 0], window=50)),
+    ("bf16", "fp8", [700], [800], 64, dict(causal=True, window=300)),
+    ("bf16", "int8", [500], [520], 32, {})])
+def test_attention_of_long_chunks(dtype, fmt, rows, lengths, dh, kw):
+    """Both sides of the numbers of rows from which keys pass through LDS."""
+    say(f"[gpu] long chunks {dtype} over {fmt}: rows {rows} lengths {lengths} dh {dh} {kw}")
+    Call(device(), dtype, fmt, rows, lengths, 1, 1, dh, seed=13, **kw).check("long chunks")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_unwritten_scales_do_not_matter_to_long_chunks(fmt):
+    dev = device()
+    c = Call(dev, "bf16", fmt, [150, 140], [200, 161], 2, 2, 128, seed=14, causal=True)
+    clean = [t.clone() for t in c.run()]
+    c.check("clean", got=clean)
+    k, v, ks, vs = c.tensors
+    unused = torch.ones((k.shape[0], 64), dtype=torch.bool)
+    for s, n in enumerate(c.lengths):
+        for p in range(n):
+            unused[M.place(c.tab, 64, s, p)] = False
+    unused = unused.to(dev)
+    for x, bad in ((ks, NAN), (vs, INF)):
+        x.permute(0, 2, 1)[unused] = bad
+    if fmt == "fp8":
+        k.permute(0, 2, 1, 3).view(torch.uint8)[unused] = 0x7f
+        v.permute(0, 3, 1, 2).view(torch.uint8)[unused] = 0xff
+    got = c.run()
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
