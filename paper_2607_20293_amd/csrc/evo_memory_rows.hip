@@ -3,7 +3,9 @@
 // and reading it back.
 //
 // What bounds it: memory.  Every value is read once and written once; norm,
-// rotation and quantising are a few operations a value.
+// rotation and quantising are a few operations a value (65537 tokens of 40 heads
+// of 128: 309 us, 4.35 TB/s of a copy's 4.92; 8 memories of 8191 fp8 tokens written
+// and read back: 160 us, 3.7 TB/s).
 //  * Queries and keys: a row of head_dim values lies over head_dim / 8 lanes,
 //    8 values a lane (16 bytes of bf16), so that the row's sum of squares or
 //    maximum takes 2 to 4 lane exchanges.  A group of lanes keeps its token's
