@@ -2,7 +2,7 @@
 // with the softmax's running maximum and sum, in one pass over the cache.
 //
 // A workgroup takes a tile of 16 R rows (tokens x the query heads that share a
-// key/value head) and a part of the keys; its four or eight waves take blocks of
+// key/value head) and a part of the keys; its one, four or eight waves take blocks of
 // 64 keys in turn and join at the end.  Products are formed transposed, S^T = K
 // Q^T and O^T = V^T P^T:
 //  * a lane of the first product's result holds one row's scores, so scaling,
@@ -575,7 +575,7 @@ template <typename T, int F, int DH, int R, int NW, bool PARTS>
 __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stream_kernel(AttArgs a) {
   typedef Lay<F, DH> L;
   constexpr int TR = 16 * R;
-  __shared__ __attribute__((aligned(16))) float join_o[NW / 2][TR * DH];
+  __shared__ __attribute__((aligned(16))) float join_o[NW > 1 ? NW / 2 : 1][NW > 1 ? TR * DH : 4];
   __shared__ float join_ml[NW][TR][2];
   // scales of a wave's block, keys' and values'
   __shared__ __attribute__((aligned(16))) float scales[is_coded(F) ? NW : 1][2][is_coded(F) ? kKeys : 4];
@@ -840,9 +840,11 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
 #pragma unroll
       for (int c = 0; c < L::CT; ++c) o[r][c] += *reinterpret_cast<const f32x4*>(src + ((r * L::CT + c) * 64 + lane) * 4);
   };
-  if (w >= NW / 2) put(join_o[w - NW / 2]);
-  __syncthreads();
-  if (w < NW / 2) add(join_o[w]);
+  if constexpr (NW > 1) {
+    if (w >= NW / 2) put(join_o[w - NW / 2]);
+    __syncthreads();
+    if (w < NW / 2) add(join_o[w]);
+  }
 #pragma unroll
   for (int k = NW / 4; k >= 1; k /= 2) {  // waves k .. 2 k - 1 use the place that they have just read
     if (w >= k && w < 2 * k) put(join_o[w]);
@@ -1372,7 +1374,9 @@ constexpr int64_t lds_rows(int f, int dh) {
 
 template <typename T, int F, int DH, int R, int NW>
 void launch_stream(int64_t wgs, const AttArgs& a, hipStream_t stream) {
-  if constexpr (NW == 4 || eight_waves(F, DH, 16 * R))
+  if constexpr (NW == 1)  // (not in parts)
+    hipLaunchKernelGGL((stream_kernel<T, F, DH, R, 1, false>), dim3(wgs), dim3(64), 0, stream, a);
+  else if constexpr (NW == 4 || eight_waves(F, DH, 16 * R))
     hipLaunchKernelGGL((a.n_split > 1 ? stream_kernel<T, F, DH, R, NW, true> : stream_kernel<T, F, DH, R, NW, false>),
                        dim3(wgs), dim3(NW * 64), 0, stream, a);
 }
@@ -1384,10 +1388,12 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
   if (p.tiles_per_seq > 1) wgs = (wgs / p.tiles_per_seq + 7) / 8 * 8 * p.tiles_per_seq;  // (see find_unit)
   constexpr int R2 = two_row_blocks(F, DH) ? 2 : 1;
   if (p.tile_rows == 16) {
-    if (p.waves == 8) launch_stream<T, F, DH, 1, 8>(wgs, a, stream);
+    if (p.waves == 1) launch_stream<T, F, DH, 1, 1>(wgs, a, stream);
+    else if (p.waves == 8) launch_stream<T, F, DH, 1, 8>(wgs, a, stream);
     else launch_stream<T, F, DH, 1, 4>(wgs, a, stream);
   } else if (p.tile_rows == 32) {
-    if (p.waves == 8) launch_stream<T, F, DH, R2, 8>(wgs, a, stream);
+    if (p.waves == 1) launch_stream<T, F, DH, R2, 1>(wgs, a, stream);
+    else if (p.waves == 8) launch_stream<T, F, DH, R2, 8>(wgs, a, stream);
     else launch_stream<T, F, DH, R2, 4>(wgs, a, stream);
   } else if constexpr (sizeof(T) == 2 && lds_rows(F, DH) != kNever) {
     if (p.tile_rows == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 4>), dim3(wgs), dim3(256), 0, stream, a);
@@ -1450,6 +1456,11 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   // a workgroup that has its compute unit to itself brings eight waves, unless its
   // part has fewer blocks than that
   p.waves = wgs * p.n_split <= n_cu && (p.n_split == 1 || blocks / p.n_split >= 8) && eight_waves(format, head_dim, p.tile_rows) ? 8 : kWaves;
+  // where tiles alone give every SIMD a wave and their keys are few, a wave takes a
+  // tile of its own: no wave without a block, no join (84 chunks of 1600 fp32 rows
+  // over 27 positions 491 us with four waves and 129 with one, int8 136 and 48;
+  // over 250 93 and 52, int8 27 and 20; over 1000 126 and 111, int8 35 and 43)
+  if (p.tile_rows <= 32 && p.n_split == 1 && wgs >= 4 * (int64_t)n_cu && blocks <= 8) p.waves = 1;
   if (p.n_split > 1) {
     p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
     p.part_floats = wgs * p.n_split * p.tile_rows * head_dim;

@@ -539,3 +539,11 @@ def test_unwritten_scales_do_not_matter_to_long_chunks(fmt):
         v.permute(0, 3, 1, 2).view(torch.uint8)[unused] = 0xff
     got = c.run()
     assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
+
+
+@pytest.mark.parametrize("dtype,fmt,rows", [("bf16", "int8", 64), ("bf16", "fp8", 60), ("fp32", "fp32", 120), ("bf16", "bf16", 60)])
+def test_many_rows_over_few_keys(dtype, fmt, rows):
+    """As many row tiles as the device has SIMDs and more: a wave takes a tile."""
+    n = 34 if rows == 64 else 70
+    lengths = [(37 * s) % 140 for s in range(n)]
+    Call(device(), dtype, fmt, [rows - s % 3 for s in range(n)], lengths, 8, 8, 64, seed=15, causal=True).check("few keys")
