@@ -609,6 +609,10 @@ class Encoder:
 
 # --------------------------------------------------------------------------
 # long memories: norm and rotation, the paged cache, attention over it
+#
+# `stream` (None: the current one) is a torch stream of the tensors' device: the
+# work goes there, and tensors made by the call belong to it.  What it has to
+# wait for, and what has to wait for it, is the caller's to say.
 # --------------------------------------------------------------------------
 class KVCacheDesc(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
@@ -704,16 +708,9 @@ _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _enqueue(device, stream, made, call, *args):
-    """call(*args, stream handle) with the device current.  Tensors made here
-    for a stream that is not the current one are kept until its work is done."""
-    if stream is None:
-        handle = _current_stream(device.index)
-    else:
-        handle = stream.cuda_stream
-        if handle != _current_stream(device.index):
-            for t in made:
-                t.record_stream(stream)
+def _enqueue(device, call, *args):
+    """call(*args, handle of the current stream) with the device current."""
+    handle = _current_stream(device.index)
     if _current_device() == device.index:
         rc = call(*args, handle)
     else:
@@ -721,6 +718,26 @@ def _enqueue(device, stream, made, call, *args):
             rc = call(*args, handle)
     if rc != 0:
         _check(rc)
+
+
+def _on_stream(stream, device, tensors, call):
+    """call() with `stream` current, so that outputs and workspaces come from
+    that stream's memory: a block of the current stream's may still be in use
+    there, by work that `stream` does not wait for.  Tensors that the call is
+    given are kept until the stream's work is done, tensors that it returns until
+    the work is done that the current stream has when they are released."""
+    if stream.device != device:
+        raise ValueError(f"stream of {stream.device}, tensors on {device}")
+    current = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        made = call()
+    if stream.cuda_stream != current.cuda_stream:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+        for t in made:
+            t.record_stream(current)
+    return made
 
 
 def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, device="cuda"):
@@ -767,6 +784,9 @@ class KVCache:
             return cls(k, v)
         return cls(k, v, *(torch.empty((n_pages, n_kv_heads, page_size), device=device) for _ in range(2)))
 
+    def tensors(self):
+        return [t for t in (self.k, self.v, self.k_scale, self.v_scale) if t is not None]
+
     def rows(self, page_table, n_rows: int, cu_rows, max_rows) -> KVRows:
         """The rows of a call (evo_kv_rows): page_table int32 [seqs][pages];
         cu_rows int32 [seqs + 1] or None (as many rows in every sequence)."""
@@ -810,6 +830,9 @@ def qk_norm_rope(q, k, positions, table, q_gain=None, k_gain=None, eps: Optional
     (float32 [n_positions][rotary_dim / 2][2]; None: not).  out: (q_out,
     k_out), which may be (q, k).  Returns (q_out, k_out)."""
     device = _device_of(q)
+    if stream is not None:
+        return _on_stream(stream, device, (q, k, positions, table, q_gain, k_gain),
+                          lambda: qk_norm_rope(q, k, positions, table, q_gain, k_gain, eps, pairs, out))
     dt, dtype = _row_dtype(q), q.dtype
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [rows][heads][dh]")
@@ -817,15 +840,13 @@ def qk_norm_rope(q, k, positions, table, q_gain=None, k_gain=None, eps: Optional
     hk = k.shape[1]
     qs, ks = (n, hq, dh), (n, hk, dh)
     nr = _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device)
-    made = ()
     if out is None:
         q_out, qo = _new(q, n, hq, dh)
         k_out, ko = _new(q, n, hk, dh)
-        made = (q_out, k_out)
     else:
         q_out, k_out = out
         qo, ko = _heads("q_out", q_out, dtype, qs, device), _heads("k_out", k_out, dtype, ks, device)
-    _enqueue(device, stream, made, lib().evo_qk_norm_rope, nr, dt, dh, n, hq, hk, _heads("q", q, dtype, qs, device),
+    _enqueue(device, lib().evo_qk_norm_rope, nr, dt, dh, n, hq, hk, _heads("q", q, dtype, qs, device),
              _heads("k", k, dtype, ks, device),
              None if table is None else _ptr("positions", positions, torch.int32, (n,), device), qo, ko)
     return q_out, k_out
@@ -835,9 +856,13 @@ def cache_write(cache: KVCache, page_table, starts, k, v, cu_rows=None, max_rows
     """evo_cache_write: k, v [rows][kv_heads][dh] into the cache, row i of
     sequence s at position starts[s] + i (int32 [sequences])."""
     device, dtype = cache.device, k.dtype
+    if stream is not None:
+        _on_stream(stream, device, (*cache.tensors(), page_table, starts, k, v, cu_rows),
+                   lambda: cache_write(cache, page_table, starts, k, v, cu_rows, max_rows) or ())
+        return
     dt, shape = _row_dtype(k), (k.shape[0], cache.n_kv_heads, cache.head_dim)
     rows = cache.rows(page_table, shape[0], cu_rows, max_rows)
-    _enqueue(device, stream, (), lib().evo_cache_write, cache.desc, rows, dt,
+    _enqueue(device, lib().evo_cache_write, cache.desc, rows, dt,
              _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), _heads("k", k, dtype, shape, device),
              _heads("v", v, dtype, shape, device))
 
@@ -847,15 +872,17 @@ def cache_read(cache: KVCache, page_table, starts, n_rows: int, dtype, cu_rows=N
     """evo_cache_read: positions starts[s] + i of every sequence as (k, v),
     [n_rows][kv_heads][dh] of dtype."""
     device, shape = cache.device, (n_rows, cache.n_kv_heads, cache.head_dim)
+    if stream is not None:
+        return _on_stream(stream, device, (*cache.tensors(), page_table, starts, cu_rows),
+                          lambda: cache_read(cache, page_table, starts, n_rows, dtype, cu_rows, max_rows, out))
     rows = cache.rows(page_table, n_rows, cu_rows, max_rows)
-    made = ()
     if out is None:
-        made = k, v = [cache.k.new_empty(*shape, dtype=dtype) for _ in range(2)]
-        ko, vo = [Heads(t.data_ptr(), shape[1] * shape[2], shape[2]) for t in made]
+        k, v = [cache.k.new_empty(*shape, dtype=dtype) for _ in range(2)]
+        ko, vo = [Heads(t.data_ptr(), shape[1] * shape[2], shape[2]) for t in (k, v)]
     else:
         k, v = out
         ko, vo = _heads("k_out", k, dtype, shape, device), _heads("v_out", v, dtype, shape, device)
-    _enqueue(device, stream, made, lib().evo_cache_read, cache.desc, rows, _row_dtype(k),
+    _enqueue(device, lib().evo_cache_read, cache.desc, rows, _row_dtype(k),
              _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), ko, vo)
     return k, v
 
@@ -867,6 +894,10 @@ def qkv_write(cache: KVCache, page_table, starts, q, k, v, table, q_gain=None, k
     normalised, rotated and written, v written; rotation by the positions
     starts[s] + i that are written."""
     device, dh, dtype = cache.device, cache.head_dim, q.dtype
+    if stream is not None:
+        return _on_stream(stream, device, (*cache.tensors(), page_table, starts, q, k, v, table, q_gain, k_gain, cu_rows),
+                          lambda: (qkv_write(cache, page_table, starts, q, k, v, table, q_gain, k_gain, eps, pairs, cu_rows,
+                                             max_rows, q_out),))[0]
     dt = _row_dtype(q)
     if q.dim() != 3:
         raise ValueError("q must be [rows][heads][dh]")
@@ -874,13 +905,11 @@ def qkv_write(cache: KVCache, page_table, starts, q, k, v, table, q_gain=None, k
     qs, ks = (n, hq, dh), (n, cache.n_kv_heads, dh)
     rows = cache.rows(page_table, n, cu_rows, max_rows)
     nr = _norm_rope(table, q_gain, k_gain, eps, pairs, dh, device)
-    made = ()
     if q_out is None:
         q_out, qo = _new(q, n, hq, dh)
-        made = (q_out,)
     else:
         qo = _heads("q_out", q_out, dtype, qs, device)
-    _enqueue(device, stream, made, lib().evo_qkv_write, cache.desc, rows, nr, dt, hq,
+    _enqueue(device, lib().evo_qkv_write, cache.desc, rows, nr, dt, hq,
              _ptr("starts", starts, torch.int32, (rows.n_seqs,), device), _heads("q", q, dtype, qs, device),
              _heads("k", k, dtype, ks, device), _heads("v", v, dtype, ks, device), qo)
     return q_out
@@ -896,11 +925,16 @@ def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_ro
     plan alone (0: the page table's).  Returns (out [rows][heads][dh], lse
     float32 [rows][heads])."""
     device, dh, dtype = cache.device, cache.head_dim, q.dtype
-    if _current_device() != device.index:  # (the plan is the current device's)
-        with torch.cuda.device(device):
+    if stream is not None or _current_device() != device.index:  # (the plan is the current device's)
+        def again():
             return chunk_attention(q, cache, page_table, lengths, cu_rows, max_rows, scale=scale, causal=causal,
                                    window=window, cap=cap, slopes=slopes, prefix=prefix, starts=starts,
-                                   max_length=max_length, out=out, lse=lse, stream=stream)
+                                   max_length=max_length, out=out, lse=lse)
+        if stream is not None:
+            return _on_stream(stream, device, (*cache.tensors(), q, page_table, lengths, cu_rows, slopes, prefix, starts),
+                              again)
+        with torch.cuda.device(device):
+            return again()
     dt = _row_dtype(q)
     if q.dim() != 3:
         raise ValueError("q must be [rows][heads][dh]")
@@ -914,16 +948,13 @@ def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_ro
                     None if prefix is None else _ptr("prefix", prefix, i32, seqs, device),
                     None if slopes is None else _ptr("slopes", slopes, torch.float32, (hq,), device))
     L, desc = lib(), cache.desc
-    made = []
     if out is None:
         out, ho = _new(q, n, hq, dh)
-        made.append(out)
     else:
         ho = _heads("out", out, dtype, qs, device)
     if lse is None:
         lse = q.new_empty(n, hq, dtype=torch.float32)
         lse_at = lse.data_ptr()
-        made.append(lse)
     else:
         lse_at = _ptr("lse", lse, torch.float32, (n, hq), device)
     need = L.evo_chunk_attention_workspace(desc, rows, att)
@@ -931,8 +962,7 @@ def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_ro
     if need:
         if need < 0:
             _check(int(need))
-        made.append(q.new_empty(need, dtype=torch.uint8))
-        work = made[-1].data_ptr()
-    _enqueue(device, stream, made, L.evo_chunk_attention, desc, rows, att, _heads("q", q, dtype, qs, device), ho, lse_at,
-             work, need)
+        space = q.new_empty(need, dtype=torch.uint8)
+        work = space.data_ptr()
+    _enqueue(device, L.evo_chunk_attention, desc, rows, att, _heads("q", q, dtype, qs, device), ho, lse_at, work, need)
     return out, lse
