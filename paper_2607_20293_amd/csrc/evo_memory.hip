@@ -347,7 +347,10 @@ int evo_chunk_attention(const evo_kv_cache* cache, const evo_kv_rows* rows, cons
   a.causal = att->causal;
   a.window = att->window;
   a.scale = att->scale;
-  a.cap = att->cap;
+  // (scores below 2^-100 are 0 to their exponential: a smaller cap's reciprocal
+  // would leave the range of floats)
+  a.cap = att->cap > 0.f ? std::fmax(att->cap, 0x1p-100f) : 0.f;
+  a.inv_cap = a.cap > 0.f ? 1.f / a.cap : 0.f;
   a.wide = is_wide(a.q, att->dtype) && is_wide(a.out, att->dtype);
   a.tiles_per_seq = p.tiles_per_seq;
   a.n_tiles = p.n_tiles;

@@ -85,7 +85,7 @@ struct AttArgs {
   const float* slopes;        // or NULL
   int n_heads, group;         // group: query heads per key/value head
   int causal, window;
-  float scale, cap;
+  float scale, cap, inv_cap;  // inv_cap: 0 with no cap
   int wide;                   // rows of q and out 16-byte aligned
   // plan
   int tiles_per_seq;          // 0: a sequence's tiles start at row / tile + sequence

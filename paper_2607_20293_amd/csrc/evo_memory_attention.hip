@@ -257,10 +257,22 @@ struct Sight {
   __device__ __forceinline__ bool all(int kb) const { return (kb >= all_lo && kb <= all_hi) || kb + kKeys <= prefix; }
 };
 
-template <typename T> __device__ __forceinline__ float squash(float x);
-// Behind bf16 products the absolute error of 2^-23 near 0 is far below theirs.
-template <> __device__ __forceinline__ float squash<__bf16>(float x) {
+// tanh from one exponential.  Its error is absolute, up to 2^-22, so a capped
+// score is off by up to 2^-22 of the cap however small the score is: behind bf16
+// products it is used up to caps of kFastCap, where that is 1.5e-5, and the terms'
+// rounding to bf16 is 256 times as much.
+constexpr float kFastCap = 64.f;
+__device__ __forceinline__ float squash_fast(float x) {
   return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_(x * (2.f * kLog2e)));
+}
+// tanh with an error relative to itself: above kFastCap, where scores may be far
+// smaller than the cap.  Near 0 an odd polynomial (Chebyshev interpolation of
+// (tanh(x) / x - 1) / x^2 in x^2, off by 1.6 * 2^-24).
+template <typename T> __device__ __forceinline__ float squash(float x);
+template <> __device__ __forceinline__ float squash<__bf16>(float x) {
+  const float y = x * x;
+  const float near = fmaf(x * y, fmaf(fmaf(fmaf(0.01799922f, y, -0.05339105f), y, 0.13330514f), y, -0.33333312f), x);
+  return fabsf(x) < 0.5f ? near : squash_fast(x);
 }
 template <> __device__ __forceinline__ float squash<float>(float x) { return tanhf(x); }
 
@@ -596,13 +608,14 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
 
   // Scores in units of log2 are off + mul x, mul > 0, with x the products by
   //   plain: one factor, inside the exponential (codes: with the key's scale)
-  //   capped: cap tanh(z / cap) = cap + 2 cap x, x = -1 / (1 + exp(2 z / cap));
-  //     its absolute error of 2^-23 cap is far below that of bf16 products
-  //   else: everything ahead of it
-  const bool capped = sizeof(T) == 2 && a.cap > 0.f && !a.slopes;
+  //   capped: cap tanh(z / cap) = cap + 2 cap x, x = -1 / (1 + exp(2 z / cap))
+  //     (squash_fast, folded into the exponential)
+  //   else: everything ahead of it; a cap's own factors one after another, because
+  //     scale / cap or cap * log2(e) may leave the range of floats
+  const bool capped = sizeof(T) == 2 && a.cap > 0.f && a.cap <= kFastCap && !a.slopes;
   const bool plain = a.cap == 0.f && !a.slopes && a.scale != 0.f;
   const float cap_log2 = a.cap * kLog2e, to_log2 = a.scale * kLog2e;
-  const float pre = capped ? 2.f * to_log2 / a.cap : a.cap > 0.f ? a.scale / a.cap : to_log2;
+  const float pre = capped ? 2.f * to_log2 * a.inv_cap : a.cap > 0.f ? a.scale : to_log2;
   const float mul = capped ? 2.f * cap_log2 : plain && !is_coded(F) ? fabsf(to_log2) : 1.f, off = capped ? cap_log2 : 0.f;
   const bool flip = plain && !is_coded(F) && a.scale < 0.f;
 
@@ -737,7 +750,7 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
         each([&](float& x, int, int) { x = __builtin_amdgcn_rcpf(-1.f - exp2_(is_coded(F) ? x : x * pre)); });
       } else if (!plain) {
         if (!is_coded(F)) each([&](float& x, int, int) { x *= pre; });
-        if (a.cap > 0.f) each([&](float& x, int, int) { x = cap_log2 * squash<T>(x); });
+        if (a.cap > 0.f) each([&](float& x, int, int) { x = a.cap * squash<T>(x * a.inv_cap) * kLog2e; });
         if (a.slopes)
           each([&](float& x, int t, int i) { x = fmaf(-slope[r], fabsf((float)(pos[r] - kb - L::key_of(t, g, i))), x); });
       }
@@ -1068,7 +1081,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   // the largest score), else ahead of it
   const bool plain = a.cap == 0.f && !a.slopes && a.scale != 0.f;
   const float factor = plain ? fabsf(a.scale) * kLog2e : 1.f;
-  const float to_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, cap_log2 = a.cap * kLog2e, to_log2 = a.scale * kLog2e;
+  const bool fast_cap = a.cap <= kFastCap;
+  const float to_cap = a.scale * a.inv_cap, cap_log2 = a.cap * kLog2e, to_log2 = a.scale * kLog2e;
   bf16x8 q[DH / 16];
   {
     const __bf16* p = reinterpret_cast<const __bf16*>(a.q.p) + (wh.row0 + tok) * a.q.row + head * a.q.head + half * 8;
@@ -1247,7 +1261,9 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             float z = s[t][e];
-            z = a.cap > 0.f ? cap_log2 * squash<__bf16>(z * to_cap) : z * to_log2;
+            z = a.cap == 0.f ? z * to_log2
+                : fast_cap   ? cap_log2 * squash_fast(z * to_cap)
+                             : a.cap * squash<__bf16>(z * a.scale * a.inv_cap) * kLog2e;
             if (a.slopes) z = fmaf(-slope, fabsf((float)(pos - key_at(t, e))), z);
             s[t][e] = z;
           }
