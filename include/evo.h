@@ -638,6 +638,8 @@ int evo_qkv_write(const evo_kv_cache* cache, const evo_kv_rows* rows, const evo_
 /* Attention of a chunk of new tokens over the cache.  Row i of sequence s is
  * at position p_i = starts[s] + i (NULL: starts[s] = lengths[s] - rows of s,
  * so the chunk is the cache's end); its keys are positions j < lengths[s].
+ * starts lie between -2^30 and 2^30 (others are taken as the nearer of these);
+ * n_rows is below 2^30.
  *   z_ij = scale q_i . k_j; cap > 0: z = cap tanh(z / cap);
  *   slopes: z = z - slopes[head] |p_i - j|
  *   visible: j < prefix[s], or

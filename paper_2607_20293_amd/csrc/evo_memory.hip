@@ -165,6 +165,7 @@ int check_attention(const evo_kv_cache* c, const evo_kv_rows* r, const evo_atten
   if (t->n_heads < 1 || t->n_heads % c->n_kv_heads)
     return fail(EVO_E_INVALID, "n_heads %d is not a multiple of the cache's %d", t->n_heads, c->n_kv_heads);
   TRY(check_rows(r, c, t->n_heads, pointers));
+  if (r->n_rows >= kMaxPositions) return fail(EVO_E_UNSUPPORTED, "rows above 2^30");
   if (t->causal != 0 && t->causal != 1) return fail(EVO_E_INVALID, "causal must be 0 or 1");
   if (t->window < 0 || t->window > kMaxPositions) return fail(EVO_E_INVALID, "window %d", t->window);
   if (t->max_length < 0) return fail(EVO_E_INVALID, "max_length %d", t->max_length);

@@ -135,9 +135,13 @@ __device__ __forceinline__ bool find_unit(const AttArgs& a, int block, int* tile
   return true;
 }
 
+// A row tile.  Positions of rows lie from -2^30 to below 2^31 - 1, the others and
+// the window from 0 to 2^30: sums and differences below stay in 32 bits in the
+// order that they are written in.
 struct Where {
   int row0, rows, base, p_first, p_last, ctx, start, prefix;
 };
+constexpr int kFar = 1 << 30;
 
 // The first row of a sequence, inside the call's rows whatever cu_rows holds.
 __device__ __forceinline__ int first_row(const RowsView& r, int seq) { return min(max(r.cu[seq], 0), r.n_rows); }
@@ -171,7 +175,7 @@ __device__ __forceinline__ bool find_tile(const AttArgs& a, int tile, int tile_r
   w->rows = n * a.group;
   w->base = j * tile_rows;
   w->ctx = min(max(a.lengths[seq], 0), a.rows.max_pages << a.cache.page_shift);
-  w->start = a.starts ? min(max(a.starts[seq], -(1 << 29)), 1 << 29) : w->ctx - n;
+  w->start = a.starts ? min(max(a.starts[seq], -kFar), kFar) : w->ctx - n;
   w->prefix = a.prefix ? min(max(a.prefix[seq], 0), w->ctx) : 0;
   w->p_first = w->start + a.by_group.divide(w->base);
   w->p_last = w->start + a.by_group.divide(min(w->base + tile_rows, w->rows) - 1);
@@ -188,7 +192,7 @@ __device__ __forceinline__ Blocks blocks_of(const AttArgs& a, const Where& w) {
   int hi = w.ctx, lo = 0;
   if (a.causal) hi = min(hi, w.p_last + 1);
   if (a.window) {
-    hi = min(hi, w.p_last + a.window);
+    hi = min(hi, min(w.p_last, w.ctx - a.window) + a.window);
     lo = max(0, w.p_first - a.window + 1);
   }
   Blocks b;
@@ -209,6 +213,8 @@ struct Pages {
   __device__ __forceinline__ int at(int i) const { return __builtin_amdgcn_readlane(held, i & 63); }
 };
 
+// |p - j|, also of a key past the cache's end (without a value that matters)
+__device__ __forceinline__ float distance(int p, int j) { return fabsf((float)(int)((unsigned)p - (unsigned)j)); }
 __device__ __forceinline__ bool sees(const AttArgs& a, const Where& w, int p, int j) {
   const bool near = (!a.causal || j <= p) && (!a.window || abs(p - j) < a.window);
   return j < w.ctx && (j < w.prefix || near);
@@ -224,7 +230,7 @@ struct Seen {
     int hi = w.ctx;
     if (a.causal) hi = min(hi, p + 1);
     if (a.window) {
-      hi = min(hi, p + a.window);
+      hi = min(hi, min(p, w.ctx - a.window) + a.window);
       lo = max(0, p - a.window + 1);
     }
     span = (unsigned)max(hi - lo, 0);
@@ -237,17 +243,17 @@ struct Seen {
 struct Sight {
   int any_lo, any_hi, all_lo, all_hi, prefix;
   __device__ __forceinline__ void set(const AttArgs& a, const Where& w) {
-    any_lo = all_lo = -(1 << 30);
-    any_hi = 1 << 30;
+    any_lo = all_lo = -kFar;
+    any_hi = kFar;
     all_hi = w.ctx - 1;
     if (a.causal) {
       any_hi = w.p_last;
       all_hi = min(all_hi, w.p_first);
     }
     if (a.window) {
-      any_hi = min(any_hi, w.p_last + a.window - 1);
-      any_lo = w.p_first - a.window + 2 - kKeys;
-      all_hi = min(all_hi, w.p_first + a.window - 1);
+      any_hi = min(any_hi, min(w.p_last, kFar) + (a.window - 1));
+      any_lo = max(w.p_first, -1) - a.window + 2 - kKeys;
+      all_hi = min(all_hi, min(w.p_first, kFar) + (a.window - 1));
       all_lo = w.p_last - a.window + 1;
     }
     all_hi -= kKeys - 1;
@@ -752,7 +758,7 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
         if (!is_coded(F)) each([&](float& x, int, int) { x *= pre; });
         if (a.cap > 0.f) each([&](float& x, int, int) { x = a.cap * squash<T>(x * a.inv_cap) * kLog2e; });
         if (a.slopes)
-          each([&](float& x, int t, int i) { x = fmaf(-slope[r], fabsf((float)(pos[r] - kb - L::key_of(t, g, i))), x); });
+          each([&](float& x, int t, int i) { x = fmaf(-slope[r], distance(pos[r], kb + L::key_of(t, g, i)), x); });
       }
       const Seen seen(a, wh, pos[r]);
       if (masked) each([&](float& x, int t, int i) { x = seen.at(kb + L::key_of(t, g, i)) ? x : -kInf; });
@@ -1264,7 +1270,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
             z = a.cap == 0.f ? z * to_log2
                 : fast_cap   ? cap_log2 * squash_fast(z * to_cap)
                              : a.cap * squash<__bf16>(z * a.scale * a.inv_cap) * kLog2e;
-            if (a.slopes) z = fmaf(-slope, fabsf((float)(pos - key_at(t, e))), z);
+            if (a.slopes) z = fmaf(-slope, distance(pos, key_at(t, e)), z);
             s[t][e] = z;
           }
       }
