@@ -652,7 +652,9 @@ int evo_qkv_write(const evo_kv_cache* cache, const evo_kv_rows* rows, const evo_
  * codes are exact in bf16; the softmax's terms are rounded to bf16 for the
  * second product), with EVO_FP32 fp32 operands.  A capped score is off by a few
  * roundings of itself whatever the cap; with EVO_BF16 and caps up to 64 by up
- * to 2^-22 of the cap instead. */
+ * to 2^-22 of the cap instead.  The weighted values are summed before they are
+ * divided by the sum of the weights: a row's sum of |v_j| over the keys that it
+ * sees should be a float. */
 typedef struct {
   int32_t dtype;           /* of q and out; pairs of formats as for evo_cache_write */
   int32_t n_heads;         /* a multiple of the cache's n_kv_heads */

@@ -765,10 +765,10 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
       float top = x[0][0];
       each([&](float& x, int, int) { top = fmaxf(top, x); });
       top = over_groups(fmaf(top, mul, off), true);
-      // the maximum moves only when scores outgrow it by 2^8: terms stay below
-      // 2^8 of the true maximum's, and the outputs are seldom rescaled
-      if (__any(!(top <= m[r] + 8.f))) {
-        const float m_new = fmaxf(m[r], top);
+      // the maximum is set 2^8 ahead when scores outgrow it: terms are at most 1,
+      // so they take no value out of range, and the outputs are seldom rescaled
+      if (__any(!(top <= m[r]))) {
+        const float m_new = fmaxf(m[r], top + 8.f);
         const float f = exp2_(m[r] - (m_new == -kInf ? 0.f : m_new));
         m[r] = m_new;
         l[r] *= f;
@@ -926,8 +926,8 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
 //  * 16-byte chunks of an LDS row are exchanged by the row's number (turn_of): a
 //    16-byte read serves lanes 0-3, 12-15 and 20-27 together, then 4-11, 16-19
 //    and 28-31 (measured), and these 16 rows meet the 16 places of 256 bytes.
-//  * The maximum moves only when a row's scores outgrow it by 2^8: terms stay
-//    below 2^8 of the true maximum's, and the outputs are seldom rescaled.
+//  * The maximum is set 2^8 ahead when a row's scores outgrow it: terms are at
+//    most 1, and the outputs are seldom rescaled.
 // What bounds it: matrix and vector units in turn (4096 tokens behind 8192, 32
 // heads over 8 of 128: 670 us, 1.03 PFLOP/s, 87% of a large library product's).
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -1288,8 +1288,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
       top = other_half(top, true) * factor;
-      if (__any(!(top <= m + 8.f))) {
-        const float m_new = fmaxf(m, top);
+      if (__any(!(top <= m))) {
+        const float m_new = fmaxf(m, top + 8.f);
         const float f = exp2_(m - (m_new == -kInf ? 0.f : m_new));
         m = m_new;
         l *= f;

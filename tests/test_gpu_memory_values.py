@@ -1,0 +1,47 @@
+"""GPU parity of chunk attention over values near the end of the floats' range."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import evo_memory as M
+from paper_2607_20293_amd import evo
+from tests.gpu_util import device, say
+from tests.memory_util import DTYPES, EPS16, EPS32, FORMATS, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+
+def _cache_of(dev, fmt, dtype, k, v, size=64):
+    """A cache that was written with k and v [keys][heads][dh], its table, and
+    what it holds in 64 bits."""
+    n, heads, dh = k.shape
+    cache = evo.KVCache.empty(-(-n // size), heads, dh, size, FORMATS[fmt], dev)
+    order = np.random.default_rng(23).permutation(cache.n_pages).astype(np.int32)[None]
+    tab = i32(order, dev)
+    evo.cache_write(cache, tab, i32([0], dev), k.to(DTYPES[dtype]).to(dev), v.to(DTYPES[dtype]).to(dev))
+    arr = [f64(t) if t is not None else None for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    return cache, tab, M.gather(*arr, order, 0, n)
+
+
+@pytest.mark.parametrize("dtype,fmt", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "int8"), ("bf16", "fp8"), ("fp32", "fp8")])
+@pytest.mark.parametrize("rows,dh,split", [(3, 64, 1), (3, 64, 0), (40, 128, 1), (200, 64, 1), (300, 128, 1)])
+def test_large_values(dtype, fmt, rows, dh, split):
+    """Values of 1e37 whose weights sum to 1: the later half of the blocks holds
+    scores 7 powers of 2 above the first half's."""
+    dev, keys = device(), 1024
+    say(f"[gpu] large values {dtype} over {fmt}: {rows} rows, dh {dh}")
+    gen = torch.Generator().manual_seed(24)
+    j = torch.arange(keys)
+    z = torch.where(j % 64 == 5, torch.where(j < keys // 2, 0.0, 4.75), -40.0)
+    k = torch.zeros(keys, 1, dh)
+    k[:, 0, 0] = z
+    v = 1e37 * (1 + torch.rand((keys, 1, dh), generator=gen))
+    cache, tab, (kk, vv) = _cache_of(dev, fmt, dtype, k, v)
+    q = torch.zeros(rows, 1, dh)
+    q[:, 0, 0] = 1
+    q = q.to(DTYPES[dtype]).to(dev)
+    out, lse = evo.chunk_attention(q, cache, tab, i32([keys], dev), scale=1.0, max_length=split)
+    want, want_lse = M.attend(f64(q), kk, vv, 0, 1.0)
+    # scores of one product; terms, sums over 16 keys and the output's rounding
+    assert np.max(np.abs(f64(out) - want)) <= 2e37 * (64 * EPS32 + (2.1 * EPS16 if dtype == "bf16" else 0))
+    assert np.max(np.abs(f64(lse) - want_lse)) <= 64 * EPS32 * 8
