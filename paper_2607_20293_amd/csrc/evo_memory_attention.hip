@@ -63,6 +63,16 @@ __device__ __forceinline__ void wave_sync() {
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Terms are exp2(x * factor - maximum) with the product and the difference
+// rounded as one.  The maximum is a rounded product: from 2^24 on it may lie
+// whole powers of 2 off the unrounded one, from 2^31 on far enough for terms of 0
+// or infinity.  There the products are rounded first, as the maximum was.
+constexpr float kCoarse = 0x1p24f;
+__device__ __forceinline__ float rounded_product(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
+}
+
 // maximum / sum over the four lanes lane % 16 of a wave
 __device__ __forceinline__ float over_groups(float x, bool maximum) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
@@ -775,9 +785,16 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
 #pragma unroll
         for (int c = 0; c < L::CT; ++c) o[r][c] *= f;
       }
-      const float shift = off - (m[r] == -kInf ? 0.f : m[r]);
+      float shift = off - (m[r] == -kInf ? 0.f : m[r]), by = mul;
+      if constexpr (!is_coded(F)) {  // (codes: scaled ahead, the factor is 1)
+        if (__builtin_expect(__any(fabsf(shift) >= kCoarse), 0)) {
+          each([&](float& x, int, int) { x = rounded_product(x, mul) + shift; });
+          by = 1.f;
+          shift = 0.f;
+        }
+      }
       float sum = 0.f;
-      each([&](float& x, int, int) { x = exp2_(fmaf(x, mul, shift)); sum += x; });
+      each([&](float& x, int, int) { x = exp2_(fmaf(x, by, shift)); sum += x; });
       l[r] += sum;
       if constexpr (is_coded(F)) {
         // (an unseen key's scale may be a NaN)
@@ -1298,13 +1315,21 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[c][e] *= f;
       }
-      const float base = m == -kInf ? 0.f : m;
+      float base = m == -kInf ? 0.f : m, by = factor;
+      if (__builtin_expect(__any(fabsf(base) >= kCoarse), 0)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[t][e] = rounded_product(s[t][e], factor) - base;
+        by = 1.f;
+        base = 0.f;
+      }
       float sum = 0.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          s[t][e] = exp2_(fmaf(s[t][e], factor, -base));
+          s[t][e] = exp2_(fmaf(s[t][e], by, -base));
           sum += s[t][e];
         }
       l += sum;

@@ -1,4 +1,5 @@
-"""GPU parity of chunk attention over values near the end of the floats' range."""
+"""GPU parity of chunk attention over values near the end of the floats' range,
+and with scores far beyond it for an exponential."""
 import numpy as np
 import pytest
 import torch
@@ -45,3 +46,30 @@ def test_large_values(dtype, fmt, rows, dh, split):
     # scores of one product; terms, sums over 16 keys and the output's rounding
     assert np.max(np.abs(f64(out) - want)) <= 2e37 * (64 * EPS32 + (2.1 * EPS16 if dtype == "bf16" else 0))
     assert np.max(np.abs(f64(lse) - want_lse)) <= 64 * EPS32 * 8
+
+
+@pytest.mark.parametrize("dtype,fmt", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "int8"), ("fp32", "fp8")])
+@pytest.mark.parametrize("rows,dh", [(3, 64), (40, 64), (200, 64), (300, 128)])
+@pytest.mark.parametrize("size", [3e2, 1e4, 3e5])
+def test_large_scores(dtype, fmt, rows, dh, size):
+    """Scores far beyond 2^32: the largest takes all, and the sum's logarithm
+    is that score."""
+    dev, keys = device(), 700
+    say(f"[gpu] large scores {dtype} over {fmt}: {rows} rows, dh {dh}, size {size:g}")
+    gen = torch.Generator().manual_seed(25)
+    k, v = torch.randn((keys, 2, dh), generator=gen) * size, torch.randn((keys, 2, dh), generator=gen)
+    cache, tab, (kk, vv) = _cache_of(dev, fmt, dtype, k, v)
+    q = (torch.randn((rows, 2, dh), generator=gen) * size).to(DTYPES[dtype]).to(dev)
+    for scale in (0.125, -0.125):
+        z = np.einsum("rhd,khd->rhk", f64(q), kk) * scale
+        order = np.sort(z, -1)
+        # rows whose second score is further off than products of dh terms in fp32 can move it
+        slack = 8 * dh * EPS32 * np.max(np.abs(f64(q)), (1, 2))[:, None] * np.max(np.abs(kk)) * dh * abs(scale)
+        clear = order[..., -1] - order[..., -2] > slack + 100
+        assert clear.mean() > 0.5
+        out, lse = evo.chunk_attention(q, cache, tab, i32([keys], dev), scale=scale)
+        best = np.argmax(z, -1)
+        want = np.stack([vv[best[:, h], h] for h in range(2)], 1)
+        err = np.abs(f64(out) - want)[clear]
+        assert np.all(err <= np.abs(want[clear]) * (EPS16 * 2.02 if dtype == "bf16" else 64 * EPS32))
+        assert np.all(np.abs(f64(lse) - order[..., -1]) <= 16 * dh * EPS32 * np.abs(f64(q)).max() * np.abs(kk).max() * dh ** 0.5 + slack)
