@@ -536,6 +536,7 @@ void evo_destroy_encoder(evo_encoder* e);
  * keys and values do not change while an action chunk is denoised (Sec. 3.4:
  * caches live for one action query), so they are written once into a paged
  * cache and attended to at every evaluated step (Eq. 1) by the chunk's tokens.
+ * These are inference operators: none has a gradient.
  *
  * The cache's memory belongs to the caller:
  *   k  [n_pages][n_kv_heads][page_size][head_dim]

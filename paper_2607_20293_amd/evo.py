@@ -613,6 +613,9 @@ class Encoder:
 # `stream` (None: the current one) is a torch stream of the tensors' device: the
 # work goes there, and tensors made by the call belong to it.  What it has to
 # wait for, and what has to wait for it, is the caller's to say.
+#
+# These are inference operators: none has a gradient.  A tensor that requires one
+# is refused while gradients are recorded, instead of its gradient being lost.
 # --------------------------------------------------------------------------
 class KVCacheDesc(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
@@ -661,6 +664,9 @@ def _row_dtype(t) -> int:
 def _wrong(name, t, dtype, shape, device):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a tensor")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise RuntimeError(f"{name} requires a gradient, and this operator has none: call it under torch.no_grad(), or "
+                           "with detached tensors")
     if t.dtype != dtype or t.device != device:
         raise TypeError(f"{name}: expected {dtype} on {device}, got {t.dtype} on {t.device}")
     if t.shape != shape:
@@ -670,7 +676,8 @@ def _wrong(name, t, dtype, shape, device):
 
 def _heads(name, t, dtype, shape, device) -> Heads:
     """A [rows][heads][dh] tensor with any row and head strides."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape:
+    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
+            or (t.requires_grad and torch.is_grad_enabled())):
         _wrong(name, t, dtype, shape, device)
     row, head, one = t.stride()
     if one != 1:
@@ -686,7 +693,7 @@ def _new(like, rows, heads, dh):
 
 def _ptr(name, t, dtype, shape, device) -> int:
     if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
-            or not t.is_contiguous()):
+            or not t.is_contiguous() or (t.requires_grad and torch.is_grad_enabled())):
         _wrong(name, t, dtype, shape, device)
     return t.data_ptr()
 
