@@ -178,8 +178,7 @@ int check_attention(const evo_kv_cache* c, const evo_kv_rows* r, const evo_atten
 AttPlan plan_of(const evo_kv_cache* c, const RowsView& r, const evo_attention* t) {
   const int64_t most = (int64_t)r.max_pages * c->page_size;
   const int64_t length = t->max_length ? (t->max_length < most ? t->max_length : most) : most;
-  return plan_attention(t->dtype, c->format, c->head_dim, t->n_heads, c->n_kv_heads, r, (int)length, t->window,
-                        t->causal != 0, compute_units());
+  return plan_attention(t->dtype, c->format, c->head_dim, t->n_heads, c->n_kv_heads, r, (int)length, compute_units());
 }
 int64_t bytes_of(const AttPlan& p) {
   return (p.part_floats + p.ml_floats) * (int64_t)sizeof(float) + p.flags * (int64_t)sizeof(unsigned long long);

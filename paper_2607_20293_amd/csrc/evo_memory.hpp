@@ -104,7 +104,7 @@ struct AttPlan {
 };
 
 AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_kv_heads, const RowsView& r,
-                       int max_length, int window, bool causal, int n_cu);
+                       int max_length, int n_cu);
 hipError_t launch_attention(int dtype, int format, int head_dim, const AttPlan& plan, const AttArgs& a,
                             hipStream_t stream);
 

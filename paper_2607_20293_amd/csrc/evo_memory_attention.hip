@@ -1388,8 +1388,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
     a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Joins a launch's parts, a thread four channels of a row.
-template <typename T, int DH>
+// Joins the parts of a launch of tile_kernel, a thread four channels of a row.
+template <int DH>
 __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
   const int wgs = tile_rows * (DH / 4) / 256;  // of a tile: tile_rows is 128 or 256
   const int th = blockIdx.x / wgs, x = (blockIdx.x - th * wgs) * 256 + threadIdx.x;
@@ -1398,7 +1398,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttArgs a, int tile_rows) {
   Where wh;
   if (tile >= a.n_tiles || !find_tile(a, tile, tile_rows, &seq, &wh)) return;
   const int r = x / (DH / 4);
-  if (wh.base + r < wh.rows) join_parts<T, DH>(a, wh, th, h, tile_rows, r, x % (DH / 4) * 4);
+  if (wh.base + r < wh.rows) join_parts<__bf16, DH>(a, wh, th, h, tile_rows, r, x % (DH / 4) * 4);
 }
 
 // Which formats take two row blocks to a wave, and what leaves a SIMD the
@@ -1445,11 +1445,10 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
   } else if constexpr (sizeof(T) == 2 && lds_rows(F, DH) != kNever) {
     if (p.tile_rows == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 4>), dim3(wgs), dim3(256), 0, stream, a);
     else if constexpr (DH == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 8>), dim3(wgs), dim3(512), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.n_split == 1) return e;
+    hipLaunchKernelGGL((join_kernel<DH>), dim3(blocks * (p.tile_rows * (DH / 4) / 256)), dim3(256), 0, stream, a, p.tile_rows);
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.n_split == 1 || p.flags) return e;
-  hipLaunchKernelGGL((join_kernel<T, DH>), dim3(blocks * (p.tile_rows * (DH / 4) / 256)), dim3(256), 0, stream, a,
-                     p.tile_rows);
   return hipGetLastError();
 }
 
@@ -1479,8 +1478,10 @@ int tile_rows_of(int dtype, int format, int head_dim, int64_t rows) {
 
 }  // namespace
 
+// (By the lengths alone: what masks hide is not considered, so parts of the keys
+// that no row sees may have workgroups that find no block.)
 AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_kv_heads, const RowsView& r,
-                       int max_length, int window, bool causal, int n_cu) {
+                       int max_length, int n_cu) {
   AttPlan p = {};
   const int group = n_heads / n_kv_heads;
   const int64_t rows = (int64_t)r.max_rows * group;  // of one sequence and key/value head
