@@ -53,7 +53,7 @@ int check_shape(const evo_kv_cache* c) {
 int check_cache(const evo_kv_cache* c) {
   TRY(check_shape(c));
   if (!c->k || !c->v) return fail(EVO_E_INVALID, "the cache's k or v is NULL");
-  const bool coded = c->format == EVO_CACHE_INT8 || c->format == EVO_CACHE_FP8;
+  const bool coded = is_coded(c->format);
   if (coded && (!c->k_scale || !c->v_scale)) return fail(EVO_E_INVALID, "an 8-bit cache needs k_scale and v_scale");
   if (!aligned(c->k, 16) || !aligned(c->v, 16) || (coded && (!aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))))
     return fail(EVO_E_INVALID, "the cache's arrays must be 16-byte aligned");

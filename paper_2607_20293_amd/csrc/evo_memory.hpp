@@ -7,7 +7,29 @@
 
 #include <cstdint>
 
+#include "evo.h"
+
 namespace evo {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// formats whose values are codes of 8 bits with a scale
+constexpr bool is_coded(int f) { return f == EVO_CACHE_INT8 || f == EVO_CACHE_FP8; }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// LDS that one wave writes and reads: its accesses are in order, the compiler
+// has to keep them so
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 // Division of n < 2^31 by a divisor that the launch knows, in five operations
 // (T. Granlund and P. Montgomery, Division by invariant integers using

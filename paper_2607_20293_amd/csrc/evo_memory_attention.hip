@@ -32,16 +32,12 @@
 namespace evo {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kKeys = 64;     // keys of a block
 constexpr int kWaves = 4;
 // Least blocks of a part of the keys, for so many workgroups without parts.  A
-// part costs a second launch to join it, which pays where few of the compute
+// part costs its join, which pays where few of the compute
 // units would work: one token over 1000 positions (4 workgroups) takes 8.6, 10.9
 // and 11.7 us with parts of 4, 8 and 16, over 4000 10.1, 11.4 and 16.5; 24 chunks
 // of 16 fp32 rows over 2500 (96) 29.4, 27.0 and 30.8; 32 chunks over 1500 int8
@@ -51,15 +47,7 @@ constexpr int kRing = 6;      // operands of a long chunk's products on their wa
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
 
-constexpr bool is_coded(int f) { return f == EVO_CACHE_INT8 || f == EVO_CACHE_FP8; }
 constexpr int size_of(int f) { return f == EVO_CACHE_FP32 ? 4 : f == EVO_CACHE_BF16 ? 2 : 1; }
-
-// LDS that one wave writes and reads: its accesses are in order, the compiler
-// has to keep them so
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -83,11 +71,6 @@ __device__ __forceinline__ float over_groups(float x, bool maximum) {
   const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
   const float b0 = __builtin_bit_cast(float, (uint32_t)b[0]), b1 = __builtin_bit_cast(float, (uint32_t)b[1]);
   return maximum ? fmaxf(b0, b1) : b0 + b1;
-}
-
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
-  return __builtin_bit_cast(uint32_t, v);
 }
 
 // four codes to bf16 (exact: codes have at most 8 significant bits)

@@ -24,10 +24,6 @@
 namespace evo {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kNone = -1;
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;     // heads whose rows a lane requests ahead
@@ -41,13 +37,6 @@ template <> struct Held<EVO_CACHE_INT8> { typedef int8_t type; };
 template <> struct Held<EVO_CACHE_FP8> { typedef uint8_t type; };
 template <> struct Held<kNone> { typedef uint8_t type; };
 
-constexpr bool is_coded(int f) { return f == EVO_CACHE_INT8 || f == EVO_CACHE_FP8; }
-
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
-  return __builtin_bit_cast(uint32_t, v);
-}
 __device__ __forceinline__ float low(uint32_t v) { return __builtin_bit_cast(float, v << 16); }
 __device__ __forceinline__ float high(uint32_t v) { return __builtin_bit_cast(float, v & 0xffff0000u); }
 
@@ -356,12 +345,6 @@ __device__ __forceinline__ char* address_of(char* p, int r) {
   const uint64_t u = (uint64_t)p;
   const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)u, r), hi = (uint32_t)__shfl((int)(uint32_t)(u >> 32), r);
   return reinterpret_cast<char*>(lo | (uint64_t)hi << 32);
-}
-// LDS that one wave writes and reads: its accesses are in order, the compiler
-// has to keep them so
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
 }
 __device__ __forceinline__ uint32_t top_of(u32x4 w, __bf16) {
   uint32_t m = 0;
