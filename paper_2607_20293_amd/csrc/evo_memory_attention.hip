@@ -1055,9 +1055,13 @@ template <int F, int DH, int NW> struct Stage {
 // of the values of block i + late: both places were last read at 2 i - 1 + 2
 // late at most, and are first read at 2 i + 2 + 2 late.  (Scales are stored with
 // the keys by the first two waves, at 2 i - 1 for block i; the softmax of block
-// i - 2 has read their place at 2 i - 2.)  With the products instead, a
+// i - 2 has read their place at 2 i - 2.)// With the products instead, a
 // 4096-token chunk behind 8192 tokens took 707 us; here 689 us.
-template <int F, int DH, int NW>
+//
+// FAR_CAP: a cap above kFastCap (of its own, because its code costs the others
+// registers: 100 tokens over 2000 bf16 positions, cap 30, 98 us with it and 82
+// without).
+template <int F, int DH, int NW, bool FAR_CAP>
 __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   typedef Stage<F, DH, NW> S;
   constexpr int TR = 32 * NW, CT = DH / 32;
@@ -1093,7 +1097,6 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
   // the largest score), else ahead of it
   const bool plain = a.cap == 0.f && !a.slopes && a.scale != 0.f;
   const float factor = plain ? fabsf(a.scale) * kLog2e : 1.f;
-  const bool fast_cap = a.cap <= kFastCap;
   const float to_cap = a.scale * a.inv_cap, cap_log2 = a.cap * kLog2e, to_log2 = a.scale * kLog2e;
   bf16x8 q[DH / 16];
   {
@@ -1273,9 +1276,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             float z = s[t][e];
-            z = a.cap == 0.f ? z * to_log2
-                : fast_cap   ? cap_log2 * squash_fast(z * to_cap)
-                             : a.cap * squash<__bf16>(z * a.scale * a.inv_cap) * kLog2e;
+            if constexpr (FAR_CAP) z = a.cap * squash<__bf16>(z * a.scale * a.inv_cap) * kLog2e;
+            else z = a.cap > 0.f ? cap_log2 * squash_fast(z * to_cap) : z * to_log2;
             if (a.slopes) z = fmaf(-slope, distance(pos, key_at(t, e)), z);
             s[t][e] = z;
           }
@@ -1432,8 +1434,11 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
     else if (p.waves == 8) launch_stream<T, F, DH, R2, 8>(wgs, a, stream);
     else launch_stream<T, F, DH, R2, 4>(wgs, a, stream);
   } else if constexpr (sizeof(T) == 2 && lds_rows(F, DH) != kNever) {
-    if (p.tile_rows == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 4>), dim3(wgs), dim3(256), 0, stream, a);
-    else if constexpr (DH == 128) hipLaunchKernelGGL((tile_kernel<F, DH, 8>), dim3(wgs), dim3(512), 0, stream, a);
+    const bool far = a.cap > kFastCap;
+    if (p.tile_rows == 128)
+      hipLaunchKernelGGL((far ? tile_kernel<F, DH, 4, true> : tile_kernel<F, DH, 4, false>), dim3(wgs), dim3(256), 0, stream, a);
+    else if constexpr (DH == 128)
+      hipLaunchKernelGGL((far ? tile_kernel<F, DH, 8, true> : tile_kernel<F, DH, 8, false>), dim3(wgs), dim3(512), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.n_split == 1) return e;
     hipLaunchKernelGGL((join_kernel<DH>), dim3(blocks * (p.tile_rows * (DH / 4) / 256)), dim3(256), 0, stream, a, p.tile_rows);
