@@ -51,16 +51,19 @@ constexpr int size_of(int f) { return f == EVO_CACHE_FP32 ? 4 : f == EVO_CACHE_B
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Terms are exp2(x * factor - maximum) with the product and the difference
+// Terms are exp2(d), d = x * factor - maximum with the product and the difference
 // rounded as one.  The maximum is a rounded product: from 2^24 on it may lie
 // whole powers of 2 off the unrounded one, from 2^31 on far enough for terms of 0
-// or infinity.  There the products are rounded first, as the maximum was (fp32
-// caches: everywhere; 16 chunks of 400 tokens over 1500 217 us, with the test for
-// it 219, without either 215).
-constexpr float kCoarse = 0x1p24f;
-__device__ __forceinline__ float rounded_product(float x, float y) {
-#pragma clang fp contract(off)
-  return x * y;
+// or infinity.  There d is made a difference of rounded products; it is asked for
+// where the maximum moves, which costs nothing between (a comparison in every
+// block: 2000 causal tokens of 8 sequences, heads of 64, 112 us, so 110).
+__device__ __forceinline__ bool is_coarse(float maximum) {
+  return __any(fabsf(maximum) >= 0x1p24f && maximum > -kInf);
+}
+// (maximum: 0 in place of -infinity, of rows that have seen nothing)
+__device__ __forceinline__ float coarse_difference(float d, float maximum) {
+  const float x = (d + maximum) - maximum;
+  return x > 0.f ? 0.f : x;  // (a NaN stays)
 }
 
 // maximum / sum over the four lanes lane % 16 of a wave
@@ -632,10 +635,12 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
   }
   f32x4 o[R][L::CT];
   float m[R], l[R];
+  bool coarse[R];  // of the whole wave: some row's maximum is
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = -kInf;
     l[r] = 0.f;
+    coarse[r] = false;
 #pragma unroll
     for (int c = 0; c < L::CT; ++c) o[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -769,21 +774,13 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
         l[r] *= f;
 #pragma unroll
         for (int c = 0; c < L::CT; ++c) o[r][c] *= f;
+        if constexpr (!is_coded(F)) coarse[r] = is_coarse(m_new);  // (codes: scaled ahead, the factor is 1)
       }
-      float shift = off - (m[r] == -kInf ? 0.f : m[r]), by = mul;
+      const float base = m[r] == -kInf ? 0.f : m[r], shift = off - base;
       float sum = 0.f;
-      if constexpr (F == EVO_CACHE_FP32) {  // (behind fp32 products the test costs more than the rounding)
-        each([&](float& x, int, int) { x = exp2_(rounded_product(x, mul) + shift); sum += x; });
-      } else {
-        if constexpr (F == EVO_CACHE_BF16) {  // (codes: scaled ahead, the factor is 1)
-          if (__builtin_expect(__any(fabsf(shift) >= kCoarse), 0)) {
-            each([&](float& x, int, int) { x = rounded_product(x, mul) + shift; });
-            by = 1.f;
-            shift = 0.f;
-          }
-        }
-        each([&](float& x, int, int) { x = exp2_(fmaf(x, by, shift)); sum += x; });
-      }
+      each([&](float& x, int, int) { x = fmaf(x, mul, shift); });
+      if (__builtin_expect(coarse[r], 0)) each([&](float& x, int, int) { x = coarse_difference(x, base); });
+      each([&](float& x, int, int) { x = exp2_(x); sum += x; });
       l[r] += sum;
       if constexpr (is_coded(F)) {
         // (an unseen key's scale may be a NaN)
@@ -1120,6 +1117,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
   float m = -kInf, l = 0.f;
+  bool coarse = false;  // of the whole wave: some row's maximum is
 
   const int krow = key_row(lr) * (DH * 2), kturn = turn_of<DH / 8>(key_row(lr)) ^ half;
   const int vrow = lr * (kKeys * 2), vturn = turn_of<kKeys / 8>(lr) ^ half;
@@ -1305,22 +1303,25 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
         for (int c = 0; c < CT; ++c)
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[c][e] *= f;
+        coarse = is_coarse(m_new);
       }
-      float base = m == -kInf ? 0.f : m, by = factor;
-      if (__builtin_expect(__any(fabsf(base) >= kCoarse), 0)) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[t][e] = rounded_product(s[t][e], factor) - base;
-        by = 1.f;
-        base = 0.f;
-      }
+      const float base = m == -kInf ? 0.f : m;
       float sum = 0.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
+        for (int e = 0; e < 16; ++e) s[t][e] = fmaf(s[t][e], factor, -base);
+      if (__builtin_expect(coarse, 0)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[t][e] = coarse_difference(s[t][e], base);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
         for (int e = 0; e < 16; ++e) {
-          s[t][e] = exp2_(fmaf(s[t][e], by, -base));
+          s[t][e] = exp2_(s[t][e]);
           sum += s[t][e];
         }
       l += sum;

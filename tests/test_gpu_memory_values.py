@@ -73,3 +73,39 @@ def test_large_scores(dtype, fmt, rows, dh, size):
         err = np.abs(f64(out) - want)[clear]
         assert np.all(err <= np.abs(want[clear]) * (EPS16 * 2.02 if dtype == "bf16" else 64 * EPS32))
         assert np.all(np.abs(f64(lse) - order[..., -1]) <= 16 * dh * EPS32 * np.abs(f64(q)).max() * np.abs(kk).max() * dh ** 0.5 + slack)
+
+
+@pytest.mark.parametrize("dtype,fmt", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "int8")])
+@pytest.mark.parametrize("rows,dh", [(16, 64), (31, 64), (100, 64), (140, 128)])
+def test_large_scores_beside_small_and_none(dtype, fmt, rows, dh):
+    """Rows of one wave whose scores are huge, ordinary, and of nothing: each is
+    what it is alone."""
+    dev, keys = device(), 300
+    gen = torch.Generator().manual_seed(28)
+    k, v = torch.randn((keys, 1, dh), generator=gen), torch.randn((keys, 1, dh), generator=gen)
+    cache, tab, (kk, vv) = _cache_of(dev, fmt, dtype, k, v)
+    q = torch.randn((rows, 1, dh), generator=gen)
+    q[::3] *= 1e12
+    q = q.to(DTYPES[dtype]).to(dev)
+    # the first third of the rows lie before all keys
+    start = -(rows // 3)
+    out, lse = evo.chunk_attention(q, cache, tab, i32([keys], dev), causal=True, starts=i32([start], dev))
+    want, want_lse = M.attend(f64(q), kk, vv, start, dh ** -0.5, causal=True)
+    none = np.arange(rows) < -start
+    assert not f64(out)[none].any() and np.isneginf(f64(lse)[none]).all() and np.isfinite(f64(lse)[~none]).all()
+    small = ~none & (np.arange(rows) % 3 != 0)
+    # dh products of at most |q| |k|, the terms' and the output's rounding
+    dz = 4 * EPS32 * dh * dh ** 0.5 * np.max(np.abs(f64(q)[small])) * np.max(np.abs(kk))
+    bound = np.max(np.abs(vv)) * (4 * dz + 4 * (keys + 64) * EPS32 + (1.01 * EPS16 if dtype == "bf16" else 0))
+    assert np.max(np.abs(f64(out) - want)[small]) <= bound
+    assert np.max(np.abs(f64(lse) - want_lse)[small]) <= 2 * dz + (keys + 64) * EPS32 + 1e-6
+    large = ~none & (np.arange(rows) % 3 == 0)
+    z = np.einsum("rhd,khd->rhk", f64(q), kk) * dh ** -0.5
+    for i in np.nonzero(large)[0]:
+        see = z[i, 0, :start + i + 1]
+        best = np.argmax(see)
+        rest = np.delete(see, best)
+        if rest.size and see[best] - np.max(rest) < 8 * dh * EPS32 * dh ** 0.5 * np.max(np.abs(f64(q)[i])) * np.max(np.abs(kk)):
+            continue
+        err = np.abs(f64(out)[i, 0] - vv[best, 0])
+        assert np.all(err <= np.abs(vv[best, 0]) * (EPS16 * 2.02 if dtype == "bf16" else 64 * EPS32)), i
