@@ -619,8 +619,15 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
   const bool capped = sizeof(T) == 2 && a.cap > 0.f && a.cap <= kFastCap && !a.slopes;
   const bool plain = a.cap == 0.f && !a.slopes && a.scale != 0.f;
   const float cap_log2 = a.cap * kLog2e, to_log2 = a.scale * kLog2e;
-  const float pre = capped ? 2.f * to_log2 * a.inv_cap : a.cap > 0.f ? a.scale : to_log2;
-  const float mul = capped ? 2.f * cap_log2 : plain && !is_coded(F) ? fabsf(to_log2) : 1.f, off = capped ? cap_log2 : 0.f;
+  // (made in vector registers, of which waves of 16 bf16 rows over parts of the keys
+  // have none to spare; over codes they stay there: in scalar ones 128 chunks of
+  // 32 tokens over fp8 took 45 us, so 43.5)
+  const auto kept = [](float x) {
+    return F == EVO_CACHE_BF16 ? __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))) : x;
+  };
+  const float pre = kept(capped ? 2.f * to_log2 * a.inv_cap : a.cap > 0.f ? a.scale : to_log2);
+  const float mul = kept(capped ? 2.f * cap_log2 : plain && !is_coded(F) ? fabsf(to_log2) : 1.f);
+  const float off = kept(capped ? cap_log2 : 0.f);
   const bool flip = plain && !is_coded(F) && a.scale < 0.f;
 
   Query<T, DH> q[R];
