@@ -552,7 +552,7 @@ void evo_destroy_encoder(evo_encoder* e);
  * Formats: fp32 and bf16 hold values; int8 and fp8 (e4m3, largest value 448)
  * hold codes of x / s rounded to nearest, ties to even, with one scale
  * s = max|x| / 127 or / 448 for each token and head (s = 0 for a row of
- * zeros).  A row that holds a NaN or an infinity gets s = NaN: it reads back
+ * zeros), quotients in 32 bits.  A row that holds a NaN or an infinity gets s = NaN: it reads back
  * as NaN and makes the outputs of the queries that see it NaN. */
 enum { EVO_CACHE_FP32 = 0, EVO_CACHE_BF16 = 1, EVO_CACHE_INT8 = 2, EVO_CACHE_FP8 = 3 };
 typedef struct {

@@ -17,9 +17,11 @@
 // block's, the next values when the second has.
 //
 // What bounds it: memory for single tokens (6 over 65001 bf16 positions, 32 heads
-// over 8 of 128: 179 us, 5.3 TB/s), the vector units for chunks over 8-bit caches
-// (conversions and softmax; 128 of 32 tokens over 1100 fp8 positions, capped: 45
-// us, 25 of them), latencies for small calls (one token over 1000: 8.6 us).
+// over 8 of 128: 179 us, 5.3 TB/s), waiting and the vector units for chunks over
+// 8-bit caches (128 of 32 tokens over 1100 fp8 positions, capped: 44 us; conversions
+// and softmax keep the vector units busy for 25 of them, and the 2 waves that a
+// SIMD holds on average wait for 40% of their time), latencies for small calls
+// (one token over 1000: 8.6 us).
 // Longer chunks of more rows share keys and values through LDS (tile_kernel).
 #include <hip/hip_runtime.h>
 
@@ -37,8 +39,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kKeys = 64;     // keys of a block
 constexpr int kWaves = 4;
 // Least blocks of a part of the keys, for so many workgroups without parts.  A
-// part costs its join, which pays where few of the compute
-// units would work: one token over 1000 positions (4 workgroups) takes 8.6, 10.9
+// part costs its join, which pays where few of the compute units would work: one
+// token over 1000 positions (4 workgroups) takes 8.6, 10.9
 // and 11.7 us with parts of 4, 8 and 16, over 4000 10.1, 11.4 and 16.5; 24 chunks
 // of 16 fp32 rows over 2500 (96) 29.4, 27.0 and 30.8; 32 chunks over 1500 int8
 // positions (128) 11.4, 11.2 and 10.4, 64 (256) 15.6 with 8 and 11.7 with 16.
@@ -939,7 +941,8 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
 //  * The maximum is set 2^8 ahead when a row's scores outgrow it: terms are at
 //    most 1, and the outputs are seldom rescaled.
 // What bounds it: matrix and vector units in turn (4096 tokens behind 8192, 32
-// heads over 8 of 128: 670 us, 1.03 PFLOP/s, 87% of a large library product's).
+// heads over 8 of 128: 655 to 740 us by card, 1.05 to 0.93 PFLOP/s, a large library
+// product's 1.18).
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // The LDS row of a block's key that matrix row r of a 32-key tile takes: bits 2
@@ -1462,7 +1465,8 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
 //  * others take two row blocks, which halves the reads (12 heads of 64 over 4000
 //    bf16 positions of 16 sequences: 64 rows 72, one block 88; 32 rows 51 and 50;
 //    32 rows of 128, grouped by four over 8000, 109 and 137; fp32, 64 rows 158
-//    and 201).  Two row blocks of fp32 keys of 128 do not fit.
+//    and 201, but 32 rows 126 and 114: there one block would be the faster).  Two
+//    row blocks of fp32 keys of 128 do not fit.
 //  * LDS pays from lds_rows() on, where a sequence's rows share enough: heads of
 //    128, bf16: 32 rows 109, LDS 113, 64 rows 140 and 119; 8-bit: 96 rows 78 and
 //    91, 128 rows 96 and 76.  Heads of 64, bf16: 64 rows 45 and 46, 80 rows 50 and
@@ -1472,7 +1476,8 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
 //    causal 81 and 85; int8 over 8000 270 and 347.
 //  * through LDS, heads of 128 take tiles of 256 (4096 rows behind 8192 659,
 //    tiles of 128 746; 64 rows, 256 to a head, 57 and 64), the others of 128
-//    (1024 rows behind 1024, 4 sequences, 51, tiles of 256 59).
+//    (1024 rows behind 1024, 4 sequences, 51, tiles of 256 59, which then are fewer
+//    than compute units; larger calls were not compared).
 int tile_rows_of(int dtype, int format, int head_dim, int64_t rows) {
   if (dtype == EVO_BF16 && rows >= lds_rows(format, head_dim)) return head_dim == 128 && rows > 128 ? 256 : 128;
   return rows <= 16 || !two_row_blocks(format, head_dim) ? 16 : 32;

@@ -83,9 +83,11 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_ca
 
 // How a row whose largest magnitude has the bits `top` is coded: code =
 // round(x / s).  The quotient comes from s's reciprocal and one residual step,
-// which gives the correctly rounded x / s, so that ties (frequent with bf16
-// inputs) fall as the definition says.  Rows near the smallest floats are
-// lifted first (lift), to keep the reciprocal finite.
+// which gives the correctly rounded x / s in 32 bits.  (Values halfway between two
+// codes, frequent with bf16 inputs, may fall to either: s is a rounded quotient
+// itself.  200000 rows of 64 in int8: all codes but those are the exact
+// quotient's.)  Rows near the smallest floats are lifted first (lift), to keep the
+// reciprocal finite.
 struct Coding {
   float s, r, d, lift;
 };
