@@ -552,8 +552,9 @@ void evo_destroy_encoder(evo_encoder* e);
  * Formats: fp32 and bf16 hold values; int8 and fp8 (e4m3, largest value 448)
  * hold codes of x / s rounded to nearest, ties to even, with one scale
  * s = max|x| / 127 or / 448 for each token and head (s = 0 for a row of
- * zeros), quotients in 32 bits.  A row that holds a NaN or an infinity gets s = NaN: it reads back
- * as NaN and makes the outputs of the queries that see it NaN. */
+ * zeros), quotients in 32 bits.  A row that holds a NaN or an infinity gets
+ * s = NaN: it reads back as NaN and makes the outputs of the queries that see it
+ * NaN. */
 enum { EVO_CACHE_FP32 = 0, EVO_CACHE_BF16 = 1, EVO_CACHE_INT8 = 2, EVO_CACHE_FP8 = 3 };
 typedef struct {
   void* k;
@@ -650,10 +651,11 @@ int evo_qkv_write(const evo_kv_cache* cache, const evo_kv_rows* rows, const evo_
  * What a row does not see does not reach its output, whatever it holds.
  * Query head h reads key/value head h / (n_heads / n_kv_heads).  Statistics
  * and sums are fp32; with EVO_BF16 the products take bf16 operands (8-bit
- * codes are exact in bf16; the softmax's terms are rounded to bf16 for the
- * second product), with EVO_FP32 fp32 operands.  A capped score is off by a few
- * roundings of itself whatever the cap; with EVO_BF16 and caps up to 64 by up
- * to 2^-22 of the cap instead.  The weighted values are summed before they are
+ * codes are exact in bf16; the softmax's terms, over 8-bit caches with the
+ * value's scale in them, are rounded to bf16 for the second product), with
+ * EVO_FP32 fp32 operands.  A capped score is off by a few roundings of itself
+ * whatever the cap; with EVO_BF16 and caps up to 64 by up to 2^-22 of the cap
+ * instead.  The weighted values are summed before they are
  * divided by the sum of the weights: a row's sum of |v_j| over the keys that it
  * sees should be a float. */
 typedef struct {
