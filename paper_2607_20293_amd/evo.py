@@ -792,6 +792,7 @@ class KVCache:
         return cls(k, v, *(torch.empty((n_pages, n_kv_heads, page_size), device=device) for _ in range(2)))
 
     def tensors(self):
+        """The cache's tensors: k, v and, of 8-bit formats, their scales."""
         return [t for t in (self.k, self.v, self.k_scale, self.v_scale) if t is not None]
 
     def rows(self, page_table, n_rows: int, cu_rows, max_rows) -> KVRows:
