@@ -541,8 +541,8 @@ void evo_destroy_encoder(evo_encoder* e);
  * The cache's memory belongs to the caller:
  *   k  [n_pages][n_kv_heads][page_size][head_dim]
  *   v  [n_pages][n_kv_heads][head_dim][page_size]
- *   k_scale, v_scale  float [n_pages][n_kv_heads][page_size], 8-bit formats
- *     only (NULL otherwise)
+ *   k_scale, v_scale  float [n_pages][n_kv_heads][page_size], 8-bit and 4-bit
+ *     formats only (NULL otherwise)
  * Values lie transposed because a cache is written once and read at every
  * step: the attention's second product then takes its operand straight from
  * memory.  Position p of a sequence lies in slot p % page_size of page
@@ -554,8 +554,14 @@ void evo_destroy_encoder(evo_encoder* e);
  * s = max|x| / 127 or / 448 for each token and head (s = 0 for a row of
  * zeros), quotients in 32 bits.  A row that holds a NaN or an infinity gets
  * s = NaN: it reads back as NaN and makes the outputs of the queries that see it
- * NaN. */
-enum { EVO_CACHE_FP32 = 0, EVO_CACHE_BF16 = 1, EVO_CACHE_INT8 = 2, EVO_CACHE_FP8 = 3 };
+ * NaN.  fp4 (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) does the same
+ * with s = max|x| / 6 and two codes in a byte, those of values 2 r (low half) and
+ * 2 r + 1 of one token, which gives the arrays
+ *   k  [n_pages][n_kv_heads][page_size][head_dim / 2]
+ *   v  [n_pages][n_kv_heads][head_dim / 2][page_size]
+ * (no byte is shared by two tokens, so that tokens are written independently).
+ * No format has the number 4. */
+enum { EVO_CACHE_FP32 = 0, EVO_CACHE_BF16 = 1, EVO_CACHE_INT8 = 2, EVO_CACHE_FP8 = 3, EVO_CACHE_FP4 = 5 };
 typedef struct {
   void* k;
   void* v;
@@ -619,7 +625,7 @@ int evo_qk_norm_rope(const evo_norm_rope* nr, int32_t dtype, int32_t head_dim, i
 /* Write keys and values (dtype EVO_FP32 or EVO_BF16) into the cache: row i of
  * sequence s at position starts[s] + i (device int32 [n_seqs]).  Rows of one
  * call must not share a slot.  A fp32 cache takes fp32 rows, a bf16 cache bf16
- * rows, the 8-bit formats both. */
+ * rows, the 8-bit and 4-bit formats both. */
 int evo_cache_write(const evo_kv_cache* cache, const evo_kv_rows* rows, int32_t dtype, const int32_t* starts,
                     const evo_heads* k, const evo_heads* v, void* hip_stream);
 
@@ -651,7 +657,7 @@ int evo_qkv_write(const evo_kv_cache* cache, const evo_kv_rows* rows, const evo_
  * What a row does not see does not reach its output, whatever it holds.
  * Query head h reads key/value head h / (n_heads / n_kv_heads).  Statistics
  * and sums are fp32; with EVO_BF16 the products take bf16 operands (8-bit
- * codes are exact in bf16; the softmax's terms, over 8-bit caches with the
+ * and 4-bit codes are exact in bf16; the softmax's terms, over such caches with the
  * value's scale in them, are rounded to bf16 for the second product), with
  * EVO_FP32 fp32 operands.  A capped score is off by a few roundings of itself
  * whatever the cap; with EVO_BF16 and caps up to 64 by up to 2^-22 of the cap

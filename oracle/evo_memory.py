@@ -6,7 +6,7 @@ from __future__ import annotations
 
 import numpy as np
 
-TOP = {"int8": 127.0, "fp8": 448.0}
+TOP = {"int8": 127.0, "fp8": 448.0, "fp4": 6.0}
 
 
 def rope_table(n_positions, rotary, theta=10000.0):
@@ -42,13 +42,32 @@ def e4m3(y):
     return np.rint(y / step) * step
 
 
+def e2m1(y):
+    """Nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with y's sign (one bit behind the
+    leading one, smallest normal 1), ties to even (|y| <= 6)."""
+    y = np.asarray(y, np.float64)
+    step = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(y), 1.0))) - 1)
+    return np.rint(y / step) * step
+
+
+def e2m1_of_bytes(b, axis):
+    """The values of bytes of two codes, side by side along `axis`."""
+    b = np.asarray(b, np.uint8)
+    both = np.stack([b & 15, b >> 4], axis=axis + 1 if axis >= 0 else axis)
+    x, m = (both >> 1) & 3, both & 1
+    y = np.where(x == 0, 0.5 * m, (2.0 + m) * 2.0 ** (x.astype(np.float64) - 2)) * np.where(both & 8, -1.0, 1.0)
+    shape = list(b.shape)
+    shape[axis] *= 2
+    return y.reshape(shape)
+
+
 def quantise(x, fmt):
     """(codes as values, scale [...]) of rows x [...][dh]."""
     x = np.asarray(x, np.float64)
     s = np.max(np.abs(x), -1) / TOP[fmt]
     bad = ~np.isfinite(x).all(-1)
     y = np.where((s > 0)[..., None] & ~bad[..., None], x, 0.0) / np.where((s > 0) & ~bad, s, 1.0)[..., None]
-    return (np.rint(y) if fmt == "int8" else e4m3(y)), np.where(bad, np.nan, s)
+    return {"int8": np.rint, "fp8": e4m3, "fp4": e2m1}[fmt](y), np.where(bad, np.nan, s)
 
 
 def place(page_table, page_size, seq, pos):

@@ -39,7 +39,7 @@ int check_head_dim(int dh) {
 // what a cache's shape says, without its pointers
 int check_shape(const evo_kv_cache* c) {
   if (!c) return fail(EVO_E_INVALID, "cache is NULL");
-  if (c->format < EVO_CACHE_FP32 || c->format > EVO_CACHE_FP8) return fail(EVO_E_INVALID, "bad cache format %d", c->format);
+  if (c->format != EVO_CACHE_FP4 && (c->format < EVO_CACHE_FP32 || c->format > EVO_CACHE_FP8)) return fail(EVO_E_INVALID, "bad cache format %d", c->format);
   TRY(check_head_dim(c->head_dim));
   if (c->n_pages < 1 || c->n_kv_heads < 1)
     return fail(EVO_E_INVALID, "cache of %d pages, %d heads", c->n_pages, c->n_kv_heads);
@@ -54,7 +54,7 @@ int check_cache(const evo_kv_cache* c) {
   TRY(check_shape(c));
   if (!c->k || !c->v) return fail(EVO_E_INVALID, "the cache's k or v is NULL");
   const bool coded = is_coded(c->format);
-  if (coded && (!c->k_scale || !c->v_scale)) return fail(EVO_E_INVALID, "an 8-bit cache needs k_scale and v_scale");
+  if (coded && (!c->k_scale || !c->v_scale)) return fail(EVO_E_INVALID, "an 8-bit or 4-bit cache needs k_scale and v_scale");
   if (!aligned(c->k, 16) || !aligned(c->v, 16) || (coded && (!aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))))
     return fail(EVO_E_INVALID, "the cache's arrays must be 16-byte aligned");
   return EVO_OK;

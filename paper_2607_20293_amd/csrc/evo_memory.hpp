@@ -15,8 +15,12 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// formats whose values are codes of 8 bits with a scale
-constexpr bool is_coded(int f) { return f == EVO_CACHE_INT8 || f == EVO_CACHE_FP8; }
+// formats whose values are codes of 8 or 4 bits with a scale
+constexpr bool is_coded(int f) { return f == EVO_CACHE_INT8 || f == EVO_CACHE_FP8 || f == EVO_CACHE_FP4; }
+// formats whose values can be a NaN or an infinity by themselves
+constexpr bool holds_nan(int f) { return f != EVO_CACHE_INT8 && f != EVO_CACHE_FP4; }
+// values in a byte of a code, of a page's row
+constexpr int per_byte(int f) { return f == EVO_CACHE_FP4 ? 2 : 1; }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

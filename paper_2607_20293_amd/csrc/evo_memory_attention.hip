@@ -68,6 +68,17 @@ __device__ __forceinline__ float coarse_difference(float d, float maximum) {
   return x > 0.f ? 0.f : x;  // (a NaN stays)
 }
 
+// The maximum of a row whose scores reach `top`, found for all rows of a wave where
+// one outgrows its own.  Over fp4 caches a row that does not keeps its maximum (and a
+// maximum that is not coarse its differences), so that no bit of its result depends on
+// the rows beside it; the other formats' rows all move.
+template <int F> __device__ __forceinline__ float next_maximum(float m, float top) {
+  return F == EVO_CACHE_FP4 && top <= m ? m : fmaxf(m, top + 8.f);
+}
+template <int F> __device__ __forceinline__ float coarse_of_row(float d, float maximum) {
+  return F == EVO_CACHE_FP4 && !(fabsf(maximum) >= 0x1p24f) ? d : coarse_difference(d, maximum);
+}
+
 // maximum / sum over the four lanes lane % 16 of a wave
 __device__ __forceinline__ float over_groups(float x, bool maximum) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
@@ -80,6 +91,23 @@ __device__ __forceinline__ float over_groups(float x, bool maximum) {
   return maximum ? fmaxf(b0, b1) : b0 + b1;
 }
 
+// two codes of fp4 (byte S of a dword), exact in either type
+template <int S> __device__ __forceinline__ uint32_t fp4_bf16(uint32_t v) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, 1.f, S));
+}
+// A dword of a value row in fp4: channels 2 c and 2 c + 1 of 4 keys.  The matrix
+// instruction wants neighbouring keys of one channel: half bytes are exchanged
+// while they are codes, two operations a channel, which leaves pairs of keys in
+// bytes 0 and 2.
+__device__ __forceinline__ uint32_t select_bits(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
+__device__ __forceinline__ uint32_t even_channel(uint32_t v) { return select_bits(0x000f000fu, v, v >> 4); }
+__device__ __forceinline__ uint32_t odd_channel(uint32_t v) { return even_channel(v >> 4); }
+__device__ __forceinline__ u32x2 channel_bf16(uint32_t v) { return u32x2{fp4_bf16<0>(v), fp4_bf16<2>(v)}; }
+// eight codes of fp4 side by side
+__device__ __forceinline__ u32x4 row_bf16(uint32_t v) {
+  return u32x4{fp4_bf16<0>(v), fp4_bf16<1>(v), fp4_bf16<2>(v), fp4_bf16<3>(v)};
+}
+
 // four codes to bf16 (exact: codes have at most 8 significant bits)
 template <int F> __device__ __forceinline__ u32x2 codes_bf16(uint32_t v) {
   if (F == EVO_CACHE_FP8)
@@ -88,6 +116,13 @@ template <int F> __device__ __forceinline__ u32x2 codes_bf16(uint32_t v) {
   return u32x2{pack2((float)(int8_t)v, (float)(int8_t)(v >> 8)), pack2((float)(int8_t)(v >> 16), (float)(int8_t)(v >> 24))};
 }
 template <int F> __device__ __forceinline__ float code_f32(uint32_t v, int e) {
+  if (F == EVO_CACHE_FP4) {
+    const auto a = e < 2   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 0)
+                   : e < 4 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 1)
+                   : e < 6 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 2)
+                           : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 3);
+    return a[e & 1];
+  }
   if (F == EVO_CACHE_FP8) {
     const auto a = e < 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(v, false) : __builtin_amdgcn_cvt_pk_f32_fp8(v, true);
     return a[e & 1];
@@ -96,16 +131,26 @@ template <int F> __device__ __forceinline__ float code_f32(uint32_t v, int e) {
 }
 
 // How a lane's share of a block lies, by format.  E: consecutive values of a
-// key row per load; KG: consecutive keys per load of a value row.
+// key row per load; KG: consecutive keys per load of a value row.  (fp4: a value
+// row of the cache is that of two channels, a byte a key.)
 template <int F, int DH> struct Lay {
-  static constexpr int SZ = size_of(F);
-  static constexpr int E = 16 / SZ < DH / 4 ? 16 / SZ : DH / 4;
+  static constexpr int SZ = size_of(F), PB = per_byte(F);
+  static constexpr int E = 16 * PB / SZ < DH / 4 ? 16 * PB / SZ : DH / 4;
+  static constexpr int EB = E * SZ / PB;         // bytes of a load of a key row
   static constexpr int KL = DH / (4 * E);        // loads of a key row
-  static constexpr int KW = DH * SZ / 16;        // dwords of a key row
+  static constexpr int KB = DH * SZ / PB;        // bytes of a key row
+  static constexpr int KW = KB / 16;             // dwords of a key row
   static constexpr int KG = 16 / SZ;
   static constexpr int VL = 16 / KG;             // loads of a value row (16 keys)
   static constexpr int VW = 4 * SZ;              // dwords of a value row
   static constexpr int CT = DH / 16;             // tiles of channels
+  static constexpr int VT = CT / PB;             // tiles of value rows
+  // The first of the four channels that a lane has of tile c.  fp4: tiles 2 i
+  // and 2 i + 1 are the even and the odd channels of 32, and are dealt into runs
+  // of four (in_runs) after the last block.
+  __device__ static constexpr int channel(int c, int g) {
+    return PB == 2 ? (c & ~1) * 16 + g * 8 + (c & 1) * 4 : c * 16 + g * 4;
+  }
   // the key (in its block) of row 4 g + i of score tile t
   __device__ static constexpr int key_of(int t, int g, int i) {
     constexpr int U = KG / 4;
@@ -327,7 +372,9 @@ __device__ __forceinline__ f32x4 score_tile(const uint32_t* k, const Query<__bf1
 #pragma unroll
   for (int j = 0; j < DH / 32; ++j) {
     u32x4 w;
-    if constexpr (is_coded(F)) {
+    if constexpr (F == EVO_CACHE_FP4) {
+      w = row_bf16(k[j]);
+    } else if constexpr (is_coded(F)) {
       const u32x2 a = codes_bf16<F>(k[2 * j]), b = codes_bf16<F>(k[2 * j + 1]);
       w = u32x4{a[0], a[1], b[0], b[1]};
     } else {
@@ -343,7 +390,8 @@ __device__ __forceinline__ f32x4 score_tile(const uint32_t* k, const Query<float
 #pragma unroll
   for (int j = 0; j < DH / 4; ++j) {
     float x;
-    if constexpr (is_coded(F)) x = code_f32<F>(k[j / 4], j & 3);
+    if constexpr (F == EVO_CACHE_FP4) x = code_f32<F>(k[j / 8], j & 7);
+    else if constexpr (is_coded(F)) x = code_f32<F>(k[j / 4], j & 3);
     else x = __builtin_bit_cast(float, k[j]);
     s = __builtin_amdgcn_mfma_f32_16x16x4f32(x, q.f[j], s, 0, 0, 0);
   }
@@ -403,7 +451,34 @@ __device__ __forceinline__ f32x4 value_tile(const uint32_t* v, const Terms<float
   return o;
 }
 
-// Values that hold a NaN or an infinity set to 0 (int8 codes hold none; a cache
+// The same for the two tiles of a tile of fp4 value rows.
+__device__ __forceinline__ void value_tiles(const uint32_t* v, const Terms<__bf16>& p, f32x4* o) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const uint32_t a = v[2 * s], b = v[2 * s + 1];
+    const u32x2 e0 = channel_bf16(even_channel(a)), e1 = channel_bf16(even_channel(b));
+    const u32x2 d0 = channel_bf16(odd_channel(a)), d1 = channel_bf16(odd_channel(b));
+    o[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{e0[0], e0[1], e1[0], e1[1]}), p.f[s], o[0], 0, 0, 0);
+    o[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{d0[0], d0[1], d1[0], d1[1]}), p.f[s], o[1], 0, 0, 0);
+  }
+}
+__device__ __forceinline__ void value_tiles(const uint32_t* v, const Terms<float>& p, f32x4* o) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(code_f32<EVO_CACHE_FP4>(v[t], 2 * i + c), p.f[t][i], o[c], 0, 0, 0);
+}
+// Even and odd channels of 32, four a lane, to eight of them side by side.
+__device__ __forceinline__ void in_runs(f32x4* o) {
+  const f32x4 e = o[0], d = o[1];
+  o[0] = f32x4{e[0], d[0], e[1], d[1]};
+  o[1] = f32x4{e[2], d[2], e[3], d[3]};
+}
+
+// Values that hold a NaN or an infinity set to 0 (int8 and fp4 codes hold none; a cache
 // that was written holds no NaN codes of fp8, unwritten memory may).
 template <int F> __device__ __forceinline__ uint32_t finite_only(uint32_t x) {
   if constexpr (F == EVO_CACHE_FP32) return (x & 0x7f800000u) == 0x7f800000u ? 0 : x;
@@ -655,19 +730,21 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
   }
 
   // byte offsets of this lane in a block's keys and values
-  const uint32_t koff = (uint32_t)((L::key_of(0, lr >> 2, lr & 3) * DH + g * L::E) * L::SZ);
+  const uint32_t koff = (uint32_t)(L::key_of(0, lr >> 2, lr & 3) * L::KB + g * L::EB);
   const uint32_t voff = (uint32_t)(((lr << ps) + g * L::KG) * L::SZ);
-  uint32_t kr[4][L::KW], vr[L::CT][L::VW];
+  uint32_t kr[4][L::KW], vr[L::VT][L::VW];
   const auto load_keys = [&](int kb, int page) {
     const int slot = kb & ((1 << ps) - 1);
     const int64_t b = (int64_t)page * a.cache.n_kv_heads + h;
-    const char* p = reinterpret_cast<const char*>(a.cache.k) + ((b << ps) + slot) * (DH * L::SZ);
+    const char* p = reinterpret_cast<const char*>(a.cache.k) + ((b << ps) + slot) * L::KB;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < L::KL; ++i) {
-        const char* s = p + koff + ((L::key_of(t, 0, 0) * DH + i * 4 * L::E) * L::SZ);
-        if constexpr (L::E * L::SZ == 16) {
+        const char* s = p + koff + (L::key_of(t, 0, 0) * L::KB + i * 4 * L::EB);
+        if constexpr (L::EB == 4) {
+          kr[t][i] = *reinterpret_cast<const uint32_t*>(s);
+        } else if constexpr (L::EB == 16) {
           const u32x4 x = *reinterpret_cast<const u32x4*>(s);
 #pragma unroll
           for (int e = 0; e < 4; ++e) kr[t][i * 4 + e] = x[e];
@@ -681,9 +758,9 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
   const auto load_values = [&](int kb, int page) {
     const int slot = kb & ((1 << ps) - 1);
     const int64_t b = (int64_t)page * a.cache.n_kv_heads + h;
-    const char* p = reinterpret_cast<const char*>(a.cache.v) + (((b * DH) << ps) + slot) * L::SZ;
+    const char* p = reinterpret_cast<const char*>(a.cache.v) + (((b * (DH / L::PB)) << ps) + slot) * L::SZ;
 #pragma unroll
-    for (int c = 0; c < L::CT; ++c)
+    for (int c = 0; c < L::VT; ++c)
 #pragma unroll
       for (int i = 0; i < L::VL; ++i) {
         const u32x4 x = *reinterpret_cast<const u32x4*>(p + voff + (((c * 16) << ps) + i * 4 * L::KG) * L::SZ);
@@ -777,7 +854,7 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
       // the maximum is set 2^8 ahead when scores outgrow it: terms are at most 1,
       // so they take no value out of range, and the outputs are seldom rescaled
       if (__any(!(top <= m[r]))) {
-        const float m_new = fmaxf(m[r], top + 8.f);
+        const float m_new = next_maximum<F>(m[r], top);
         const float f = exp2_(m[r] - (m_new == -kInf ? 0.f : m_new));
         m[r] = m_new;
         l[r] *= f;
@@ -799,17 +876,22 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
       terms[r].set(x);
     }
     bool bad = false;
-    if (masked && __any(any_not_finite<F>(vr))) {
-      // What a row does not see must not reach it, but 0 times a NaN or an
-      // infinity is NaN: those are taken out of the operand, and added below
-      // to the rows that see them.
-      bad = clear_tail<F, DH>(vr, g, wh.ctx - kb);
+    if constexpr (holds_nan(F)) {
+      if (masked && __any(any_not_finite<F>(vr))) {
+        // What a row does not see must not reach it, but 0 times a NaN or an
+        // infinity is NaN: those are taken out of the operand, and added below
+        // to the rows that see them.
+        bad = clear_tail<F, DH>(vr, g, wh.ctx - kb);
+      }
     }
 #pragma unroll
-    for (int c = 0; c < L::CT; ++c)
+    for (int c = 0; c < L::VT; ++c)
 #pragma unroll
-      for (int r = 0; r < R; ++r) o[r][c] = value_tile<F>(vr[c], terms[r], o[r][c]);
-    if constexpr (F != EVO_CACHE_INT8) {
+      for (int r = 0; r < R; ++r) {
+        if constexpr (F == EVO_CACHE_FP4) value_tiles(vr[c], terms[r], &o[r][2 * c]);
+        else o[r][c] = value_tile<F>(vr[c], terms[r], o[r][c]);
+      }
+    if constexpr (holds_nan(F)) {
       if (__builtin_expect(__any(bad), 0)) {
 #pragma unroll 1
         for (int j = 0; j < min(kKeys, wh.ctx - kb); ++j) {
@@ -833,6 +915,13 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
     __builtin_amdgcn_sched_barrier(0);
     if (next >= 0) load_values(next, page);
     __builtin_amdgcn_sched_barrier(0);
+  }
+
+  if constexpr (F == EVO_CACHE_FP4) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int c = 0; c < L::CT; c += 2) in_runs(&o[r][c]);
   }
 
   // ---- the waves' results, in pairs: w and w + NW / 2, then w and w + NW / 4, .. ----
@@ -898,7 +987,7 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
           // states before the data's next change are left out)
 #pragma unroll
           for (int c = 0; c < L::CT; ++c)
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o[r][c]), parts.o, (part * DH + c * 16 + g * 4) * 4, 0, kCoherent);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o[r][c]), parts.o, (part * DH + L::channel(c, g)) * 4, 0, kCoherent);
         }
       }
       const bool complete = parts_complete(a, th, split);
@@ -921,7 +1010,7 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
     T* dst = reinterpret_cast<T*>(a.out.p) + (wh.row0 + tok) * a.out.row + head * a.out.head;
 #pragma unroll
     for (int c = 0; c < L::CT; ++c)
-      store4(dst + c * 16 + g * 4, a.wide, total[r] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[r][c] * inv);
+      store4(dst + L::channel(c, g), a.wide, total[r] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[r][c] * inv);
     if (a.lse && g == 0)
       a.lse[(int64_t)(wh.row0 + tok) * a.n_heads + head] =
           total[r] == 0.f ? -kInf : (top[r] + __builtin_amdgcn_logf(total[r])) * kLn2;
@@ -962,10 +1051,11 @@ __device__ __forceinline__ float other_half(float x, bool maximum) {
 // keys and of a block's values.  Where they lie is the same for every block but
 // for the block's base, which all threads share: offsets are made once.
 template <int F, int DH, int NW> struct Stage {
-  static constexpr int SZ = size_of(F), TH = NW * 64;
-  static constexpr int KC = kKeys * DH * SZ / 16;       // chunks of a block's keys, as many of its values
+  static constexpr int SZ = size_of(F), PB = per_byte(F), TH = NW * 64;
+  static constexpr int KC = kKeys * DH * SZ / PB / 16;  // chunks of a block's keys, as many of its values
   static constexpr int IT = (KC + TH - 1) / TH;
-  static constexpr int KROW = DH * SZ / 16, VROW = kKeys * SZ / 16;
+  static constexpr int KROW = DH * SZ / PB / 16, VROW = kKeys * SZ / 16;
+  static constexpr int PER = SZ == 1 ? 2 * PB : 1;      // places of a chunk in LDS, 8 values each
   static constexpr int KB = kKeys * DH * 2;             // bytes of a block's keys in LDS
   // a thread's chunks lie so many rows apart, a multiple of 16, so that they
   // are exchanged alike
@@ -973,7 +1063,7 @@ template <int F, int DH, int NW> struct Stage {
   static_assert(IT == 1 || (KSTEP % 16 == 0 && VSTEP % 16 == 0), "turn_of of a thread's chunks");
   u32x4 k[IT], v[IT];
   float scale;
-  uint32_t vat, kto[2], vto[2];  // from: values in memory; to: LDS, one 16-byte place for each 8 values
+  uint32_t vat, kto[PER], vto[PER];  // from: values in memory; to: LDS
   bool has_k, has_v;
 
   __device__ __forceinline__ void init(int ps) {
@@ -982,11 +1072,12 @@ template <int F, int DH, int NW> struct Stage {
     has_k = KC % TH == 0 || kc < (uint32_t)KC;
     has_v = KC % TH == 0 || vc < (uint32_t)KC;
     vat = ((vc / VROW) << ps) * SZ + vc % VROW * 16;
-    constexpr int PER = 16 / (8 * SZ) ? 16 / (8 * SZ) : 1;  // places of a chunk
+    constexpr int VP = PER / PB;                        // of a chunk of one channel's values
 #pragma unroll
     for (int b = 0; b < PER; ++b) {
       kto[b] = kc / KROW * (DH * 2) + ((kc % KROW * PER + b) ^ turn_of<DH / 8>(kc / KROW)) * 16;
-      vto[b] = vc / VROW * (kKeys * 2) + ((vc % VROW * PER + b) ^ turn_of<kKeys / 8>(vc / VROW)) * 16;
+      const uint32_t row = vc / VROW * PB + b / VP;
+      vto[b] = row * (kKeys * 2) + ((vc % VROW * VP + b % VP) ^ turn_of<kKeys / 8>(row)) * 16;
     }
   }
   // p, ks, vs: the block's base, the same for all threads
@@ -1002,8 +1093,11 @@ template <int F, int DH, int NW> struct Stage {
     for (int i = 0; i < IT; ++i)
       if (has_v) v[i] = *reinterpret_cast<const u32x4*>(p + (size_t)((uint32_t)(i * VSTEP) << ps) * SZ + vat);
   }
-  __device__ __forceinline__ static void put(char* lds, const uint32_t (&to)[2], u32x4 x) {
-    if constexpr (is_coded(F)) {
+  __device__ __forceinline__ static void put(char* lds, const uint32_t (&to)[PER], u32x4 x) {
+    if constexpr (F == EVO_CACHE_FP4) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) *reinterpret_cast<u32x4*>(lds + to[b]) = row_bf16(x[b]);
+    } else if constexpr (is_coded(F)) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const u32x2 lo = codes_bf16<F>(x[2 * b]), hi = codes_bf16<F>(x[2 * b + 1]);
@@ -1023,11 +1117,26 @@ template <int F, int DH, int NW> struct Stage {
   __device__ __forceinline__ void store_values(char* lds) const {
 #pragma unroll
     for (int i = 0; i < IT; ++i)
-      if (has_v) put(lds + i * VSTEP * (kKeys * 2), vto, v[i]);
+      if (has_v) {
+        char* to = lds + i * VSTEP * PB * (kKeys * 2);
+        if constexpr (F == EVO_CACHE_FP4) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const u32x2 e0 = channel_bf16(even_channel(v[i][2 * b])), e1 = channel_bf16(even_channel(v[i][2 * b + 1]));
+            const u32x2 d0 = channel_bf16(odd_channel(v[i][2 * b])), d1 = channel_bf16(odd_channel(v[i][2 * b + 1]));
+            *reinterpret_cast<u32x4*>(to + vto[b]) = u32x4{e0[0], e0[1], e1[0], e1[1]};
+            *reinterpret_cast<u32x4*>(to + vto[2 + b]) = u32x4{d0[0], d0[1], d1[0], d1[1]};
+          }
+        } else {
+          put(to, vto, v[i]);
+        }
+      }
   }
   // Values of a block that some row does not see all of: past the `left` keys
   // that the cache holds they become 0; NaNs and infinities too, and *bad is set.
+  // (fp4: finite whatever the codes are, so that terms of 0 are enough.)
   __device__ __forceinline__ void clear_values(int left, int* bad) {
+    if constexpr (F == EVO_CACHE_FP4) return;
     bool found = false;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
@@ -1038,7 +1147,7 @@ template <int F, int DH, int NW> struct Stage {
 #pragma unroll
         for (int e = 0; e < 4 / SZ; ++e)
           if (key + d * (4 / SZ) + e >= left) x &= ~(((1u << (8 * SZ)) - 1) << (8 * SZ * e));
-        if constexpr (F != EVO_CACHE_INT8) {
+        if constexpr (holds_nan(F)) {
           const uint32_t y = finite_only<F>(x);
           found |= y != x;
           x = y;
@@ -1156,12 +1265,12 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
     if (i >= n) return;
     at_keys = place(i);
     const int64_t key = at_keys.first + at_keys.slot * DH, row = at_keys.first / DH + at_keys.slot;
-    next.load_keys(reinterpret_cast<const char*>(a.cache.k) + key * S::SZ, is_coded(F) ? a.cache.ks + row : nullptr,
+    next.load_keys(reinterpret_cast<const char*>(a.cache.k) + key * S::SZ / S::PB, is_coded(F) ? a.cache.ks + row : nullptr,
                    is_coded(F) ? a.cache.vs + row : nullptr);
   };
   const auto fetch_values = [&](int i) {
     if (i >= n) return;
-    next.load_values(reinterpret_cast<const char*>(a.cache.v) + (at_values.first + at_values.slot) * S::SZ, ps);
+    next.load_values(reinterpret_cast<const char*>(a.cache.v) + (at_values.first / S::PB + at_values.slot) * S::SZ, ps);
   };
   const auto put_keys = [&](int i) {
     if (i < n) next.store_keys(lds_k[i & 1], scales[is_coded(F) ? i & 1 : 0]);
@@ -1233,7 +1342,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
     f32x16 s[2];
     products(s, p, lds_k[i & 1], lds_v[(i - 1) & 1]);
     if (i > 0) {
-      if constexpr (F != EVO_CACHE_INT8) {
+      if constexpr (holds_nan(F)) {
         if (__builtin_expect(bad[(i - 1) & 3], 0)) {
           // the values that store_values() took out, for the rows that see them
           const int kl = bl.at(v0 + i - 1) * kKeys, s0 = kl & ((1 << ps) - 1);
@@ -1305,7 +1414,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
       top = other_half(top, true) * factor;
       if (__any(!(top <= m))) {
-        const float m_new = fmaxf(m, top + 8.f);
+        const float m_new = next_maximum<F>(m, top);
         const float f = exp2_(m - (m_new == -kInf ? 0.f : m_new));
         m = m_new;
         l *= f;
@@ -1325,7 +1434,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_kernel(AttArgs a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[t][e] = coarse_difference(s[t][e], base);
+          for (int e = 0; e < 16; ++e) s[t][e] = coarse_of_row<F>(s[t][e], base);
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -1534,9 +1643,11 @@ hipError_t launch_attention(int dtype, int format, int head_dim, const AttPlan& 
   X(EVO_FP32, float, EVO_CACHE_FP32, DH)  \
   X(EVO_FP32, float, EVO_CACHE_INT8, DH)  \
   X(EVO_FP32, float, EVO_CACHE_FP8, DH)   \
+  X(EVO_FP32, float, EVO_CACHE_FP4, DH)   \
   X(EVO_BF16, __bf16, EVO_CACHE_BF16, DH) \
   X(EVO_BF16, __bf16, EVO_CACHE_INT8, DH) \
-  X(EVO_BF16, __bf16, EVO_CACHE_FP8, DH)
+  X(EVO_BF16, __bf16, EVO_CACHE_FP8, DH)  \
+  X(EVO_BF16, __bf16, EVO_CACHE_FP4, DH)
   Y(32) Y(64) Y(128)
 #undef Y
 #undef X

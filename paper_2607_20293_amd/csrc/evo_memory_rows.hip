@@ -35,6 +35,7 @@ template <> struct Held<EVO_CACHE_FP32> { typedef float type; };
 template <> struct Held<EVO_CACHE_BF16> { typedef __bf16 type; };
 template <> struct Held<EVO_CACHE_INT8> { typedef int8_t type; };
 template <> struct Held<EVO_CACHE_FP8> { typedef uint8_t type; };
+template <> struct Held<EVO_CACHE_FP4> { typedef uint8_t type; };  // two codes
 template <> struct Held<kNone> { typedef uint8_t type; };
 
 __device__ __forceinline__ float low(uint32_t v) { return __builtin_bit_cast(float, v << 16); }
@@ -91,8 +92,9 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_ca
 struct Coding {
   float s, r, d, lift;
 };
+constexpr float largest(int f) { return f == EVO_CACHE_INT8 ? 127.f : f == EVO_CACHE_FP8 ? 448.f : 6.f; }
 template <int F> __device__ __forceinline__ Coding coding_of(uint32_t top) {
-  constexpr float M = F == EVO_CACHE_INT8 ? 127.f : 448.f;
+  constexpr float M = largest(F);
   const float amax = __builtin_bit_cast(float, top);
   Coding c;
   if (top >= 0x7f800000u) {  // a NaN or an infinity in the row
@@ -107,7 +109,7 @@ template <int F> __device__ __forceinline__ Coding coding_of(uint32_t top) {
   return c;
 }
 template <int F> __device__ __forceinline__ float quotient(float x, const Coding& c) {
-  constexpr float M = F == EVO_CACHE_INT8 ? 127.f : 448.f;
+  constexpr float M = largest(F);
   if (c.r == 0.f) return 0.f;
   x *= c.lift;
   const float q = x * c.r;
@@ -134,6 +136,30 @@ template <int F> __device__ __forceinline__ void decode4(uint32_t v, float* y) {
   }
 }
 
+// The codes of 8 values, and the values of such codes: 8 bytes, or the 4 of fp4
+// (then in w[0]).
+template <int F> __device__ __forceinline__ u32x2 code8(const float* y) {
+  if constexpr (F == EVO_CACHE_FP4) {
+    uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, y[0], y[1], 1.f, 0);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[2], y[3], 1.f, 1);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[4], y[5], 1.f, 2);
+    return u32x2{__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[6], y[7], 1.f, 3), 0};
+  } else {
+    return u32x2{code4<F>(y), code4<F>(y + 4)};
+  }
+}
+template <int F> __device__ __forceinline__ void decode8(u32x2 w, float* y) {
+  if constexpr (F == EVO_CACHE_FP4) {
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], 1.f, 1),
+               c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], 1.f, 3);
+    y[0] = a[0]; y[1] = a[1]; y[2] = b[0]; y[3] = b[1];
+    y[4] = c[0]; y[5] = c[1]; y[6] = d[0]; y[7] = d[1];
+  } else {
+    decode4<F>(w[0], y);
+    decode4<F>(w[1], y + 4);
+  }
+}
+
 // Slot of position `pos` of a sequence: index of its (page, head) block, or -1
 // where there is none.
 __device__ __forceinline__ int64_t block_of(const RowsArgs& a, int seq, int pos, int head) {
@@ -154,19 +180,21 @@ template <int F, int DH>
 __device__ __forceinline__ void store_held(const RowsArgs& a, int64_t block, int slot, bool value, int lane, const float* y,
                                            const Coding& c) {
   typedef typename Held<F>::type H;
+  constexpr int BW = DH / per_byte(F), N = 8 / per_byte(F);  // elements of a row, of a lane
   const int ps = a.cache.page_shift;
-  H* k = reinterpret_cast<H*>(a.cache.k) + ((block << ps) + slot) * DH + lane * 8;
-  H* v = reinterpret_cast<H*>(a.cache.v) + ((block * DH + lane * 8) << ps) + slot;
+  H* k = reinterpret_cast<H*>(a.cache.k) + ((block << ps) + slot) * BW + lane * N;
+  H* v = reinterpret_cast<H*>(a.cache.v) + ((block * BW + lane * N) << ps) + slot;
   if constexpr (is_coded(F)) {
     float z[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] = quotient<F>(y[e], c);
-    const u32x2 w = {code4<F>(z), code4<F>(z + 4)};
+    const u32x2 w = code8<F>(z);
     if (!value) {
-      *reinterpret_cast<u32x2*>(k) = w;
+      if constexpr (N == 4) *reinterpret_cast<uint32_t*>(k) = w[0];
+      else *reinterpret_cast<u32x2*>(k) = w;
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[(int64_t)e << ps] = (H)(w[e / 4] >> (8 * (e & 3)));
+      for (int e = 0; e < N; ++e) v[(int64_t)e << ps] = (H)(w[e / 4] >> (8 * (e & 3)));
     }
     if (lane == 0) scales_of(a, value)[(block << ps) + slot] = c.s;
   } else if constexpr (F != kNone) {
@@ -421,7 +449,8 @@ __device__ __forceinline__ void v_rows(const RowsArgs& a, int block, char* lds, 
     cd = coding_of<F>(tops[lane]);
     if (live) a.cache.vs[(r.block << a.cache.page_shift) + r.slot] = cd.s;
   }
-  H* dst = reinterpret_cast<H*>(a.cache.v) + ((r.block * DH) << a.cache.page_shift) + r.slot;
+  constexpr int PB = per_byte(F);
+  H* dst = reinterpret_cast<H*>(a.cache.v) + ((r.block * (DH / PB)) << a.cache.page_shift) + r.slot;
 #pragma unroll
   for (int c = 0; c < S::C; ++c) {
     wave_sync();
@@ -437,10 +466,10 @@ __device__ __forceinline__ void v_rows(const RowsArgs& a, int block, char* lds, 
         if constexpr (is_coded(F)) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = quotient<F>(x[e], cd);
-          const uint32_t v[2] = {code4<F>(x), code4<F>(x + 4)};
+          const u32x2 v = code8<F>(x);
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            dst[(int64_t)(c * S::V + j + e) << a.cache.page_shift] = (H)(v[e / 4] >> (8 * (e & 3)));
+          for (int e = 0; e < 8 / PB; ++e)
+            dst[(int64_t)((c * S::V + j) / PB + e) << a.cache.page_shift] = (H)(v[e / 4] >> (8 * (e & 3)));
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) dst[(int64_t)(c * S::V + j + e) << a.cache.page_shift] = (H)x[e];
@@ -463,7 +492,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(RowsArgs a) {
 template <typename T, int F, int DH>
 __device__ __forceinline__ void read_keys(const RowsArgs& a, int block) {
   typedef typename Held<F>::type H;
-  constexpr int LPR = DH / 8;
+  constexpr int LPR = DH / 8, BW = DH / per_byte(F), N = 8 / per_byte(F);
   const int ps = a.cache.page_shift, groups = a.head_groups;
   const int lane = threadIdx.x % LPR;
   const int at = a.by_groups.divide(block);
@@ -479,19 +508,19 @@ __device__ __forceinline__ void read_keys(const RowsArgs& a, int block) {
     float x[8] = {};
     if (b >= 0) {
       const int64_t row = ((b + hk) << ps) + (pos & ((1 << ps) - 1));
-      const H* k = reinterpret_cast<const H*>(a.cache.k) + row * DH + lane * 8;
-      const H* v = reinterpret_cast<const H*>(a.cache.v) + (((b + hk) * DH + lane * 8) << ps) + (pos & ((1 << ps) - 1));
+      const H* k = reinterpret_cast<const H*>(a.cache.k) + row * BW + lane * N;
+      const H* v = reinterpret_cast<const H*>(a.cache.v) + (((b + hk) * BW + lane * N) << ps) + (pos & ((1 << ps) - 1));
       if constexpr (is_coded(F)) {
         u32x2 w = {0, 0};
         if (!is_v) {
-          w = *reinterpret_cast<const u32x2*>(k);
+          if constexpr (N == 4) w[0] = *reinterpret_cast<const uint32_t*>(k);
+          else w = *reinterpret_cast<const u32x2*>(k);
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(uint8_t)v[(int64_t)e << ps] << (8 * (e & 3));
+          for (int e = 0; e < N; ++e) w[e / 4] |= (uint32_t)(uint8_t)v[(int64_t)e << ps] << (8 * (e & 3));
         }
         const float s = scales_of(a, is_v)[row];
-        decode4<F>(w[0], x);
-        decode4<F>(w[1], x + 4);
+        decode8<F>(w, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] *= s;
       } else if (!is_v) {
@@ -515,7 +544,8 @@ __device__ __forceinline__ void read_values(const RowsArgs& a, int block, char* 
   const ValueRow r = value_row(a, block);
   const uint64_t rows = __ballot(r.live);
   char* dst = a.v.p + (r.n * a.v.row + r.h * a.v.head) * (int64_t)sizeof(T);
-  const H* src = reinterpret_cast<const H*>(a.cache.v) + ((r.block * DH) << ps) + r.slot;
+  constexpr int PB = per_byte(F);
+  const H* src = reinterpret_cast<const H*>(a.cache.v) + ((r.block * (DH / PB)) << ps) + r.slot;
   float s = 0.f;
   if constexpr (is_coded(F)) s = r.block >= 0 ? a.cache.vs[(r.block << ps) + r.slot] : 0.f;
 #pragma unroll
@@ -525,13 +555,12 @@ __device__ __forceinline__ void read_values(const RowsArgs& a, int block, char* 
     for (int j = 0; j < S::V; j += 8) {
       float x[8] = {};
       if (r.block >= 0) {
-        const H* p = src + ((int64_t)(c * S::V + j) << ps);
+        const H* p = src + ((int64_t)((c * S::V + j) / PB) << ps);
         if constexpr (is_coded(F)) {
-          uint32_t v[2] = {0, 0};
+          u32x2 v = {0, 0};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e / 4] |= (uint32_t)(uint8_t)p[(int64_t)e << ps] << (8 * (e & 3));
-          decode4<F>(v[0], x);
-          decode4<F>(v[1], x + 4);
+          for (int e = 0; e < 8 / PB; ++e) v[e / 4] |= (uint32_t)(uint8_t)p[(int64_t)e << ps] << (8 * (e & 3));
+          decode8<F>(v, x);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] *= s;
         } else {
@@ -604,9 +633,11 @@ hipError_t launch_read_as(RowsArgs a, hipStream_t stream) {
   X(EVO_FP32, float, EVO_CACHE_FP32, DH)  \
   X(EVO_FP32, float, EVO_CACHE_INT8, DH)  \
   X(EVO_FP32, float, EVO_CACHE_FP8, DH)   \
+  X(EVO_FP32, float, EVO_CACHE_FP4, DH)   \
   X(EVO_BF16, __bf16, EVO_CACHE_BF16, DH) \
   X(EVO_BF16, __bf16, EVO_CACHE_INT8, DH) \
-  X(EVO_BF16, __bf16, EVO_CACHE_FP8, DH)
+  X(EVO_BF16, __bf16, EVO_CACHE_FP8, DH)  \
+  X(EVO_BF16, __bf16, EVO_CACHE_FP4, DH)
 
 }  // namespace
 

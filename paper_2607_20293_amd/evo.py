@@ -645,7 +645,7 @@ class Attention(ctypes.Structure):
                 ("prefix", ctypes.c_void_p), ("slopes", ctypes.c_void_p)]
 
 
-CACHE_FP32, CACHE_BF16, CACHE_INT8, CACHE_FP8 = 0, 1, 2, 3
+CACHE_FP32, CACHE_BF16, CACHE_INT8, CACHE_FP8, CACHE_FP4 = 0, 1, 2, 3, 5
 _PAIRS = {"halves": 0, "adjacent": 1}
 
 
@@ -759,13 +759,15 @@ class KVCache:
     """A paged cache of keys and values around the caller's tensors (see
     evo_kv_cache in include/evo.h):
       k [pages][heads][page_size][dh], v [pages][heads][dh][page_size]
-    of float32, bfloat16, int8 or float8_e4m3fn; 8-bit caches also have
+    of float32, bfloat16, int8 or float8_e4m3fn, or
+      k [pages][heads][page_size][dh / 2], v [pages][heads][dh / 2][page_size]
+    of float4_e2m1fn_x2 (two values an element); 8-bit and 4-bit caches also have
     k_scale and v_scale, float32 [pages][heads][page_size]."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         device = _device_of(k)
         formats = {torch.float32: CACHE_FP32, torch.bfloat16: CACHE_BF16, torch.int8: CACHE_INT8,
-                   torch.float8_e4m3fn: CACHE_FP8}
+                   torch.float8_e4m3fn: CACHE_FP8, torch.float4_e2m1fn_x2: CACHE_FP4}
         if k.dtype not in formats:
             raise TypeError(f"no cache format holds {k.dtype}")
         if k.dim() != 4:
@@ -774,10 +776,11 @@ class KVCache:
         kp, vp = _ptr("k", k, k.dtype, k.shape, device), _ptr("v", v, k.dtype, (pages, heads, dh, size), device)
         fmt = formats[k.dtype]
         if (fmt >= CACHE_INT8) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
-            raise ValueError("8-bit caches have scales, the others have none")
+            raise ValueError("8-bit and 4-bit caches have scales, the others have none")
         ks, vs = (None if t is None else _ptr(n, t, torch.float32, (pages, heads, size), device)
                   for n, t in (("k_scale", k_scale), ("v_scale", v_scale)))
         self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, device
+        dh *= 2 if fmt == CACHE_FP4 else 1
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pages, heads, size, dh
         self.desc = KVCacheDesc(kp, vp, ks, vs, fmt, pages, size, heads, dh)
 
@@ -785,14 +788,17 @@ class KVCache:
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 64, dtype=None, device="cuda"):
         """An unwritten cache of its own tensors (dtype: bfloat16 by default)."""
         dtype = torch.bfloat16 if dtype is None else dtype
-        k = torch.empty((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
-        v = torch.empty((n_pages, n_kv_heads, head_dim, page_size), dtype=dtype, device=device)
-        if dtype not in (torch.int8, torch.float8_e4m3fn):
+        if dtype == torch.float4_e2m1fn_x2 and head_dim % 2:
+            raise ValueError(f"head_dim {head_dim} is not whole elements of {dtype}")
+        wide = head_dim // 2 if dtype == torch.float4_e2m1fn_x2 else head_dim
+        k = torch.empty((n_pages, n_kv_heads, page_size, wide), dtype=dtype, device=device)
+        v = torch.empty((n_pages, n_kv_heads, wide, page_size), dtype=dtype, device=device)
+        if dtype not in (torch.int8, torch.float8_e4m3fn, torch.float4_e2m1fn_x2):
             return cls(k, v)
         return cls(k, v, *(torch.empty((n_pages, n_kv_heads, page_size), device=device) for _ in range(2)))
 
     def tensors(self):
-        """The cache's tensors: k, v and, of 8-bit formats, their scales."""
+        """The cache's tensors: k, v and, of 8-bit and 4-bit formats, their scales."""
         return [t for t in (self.k, self.v, self.k_scale, self.v_scale) if t is not None]
 
     def rows(self, page_table, n_rows: int, cu_rows, max_rows) -> KVRows:
