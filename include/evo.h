@@ -690,6 +690,75 @@ int evo_chunk_attention(const evo_kv_cache* cache, const evo_kv_rows* rows, cons
                         const evo_heads* q, const evo_heads* out, float* lse, void* workspace, size_t workspace_bytes,
                         void* hip_stream);
 
+/* ---- Layers around the attention ---------------------------------------
+ * What a policy's layer has beside its attention: products with its weights, held
+ * in 4 bits, and the norms before and after a block with its gate and residual.
+ * Inference operators like the ones above; asynchronous on hip_stream, device
+ * memory of the current device, no workspace.
+ *
+ * A matrix [rows][columns]: row stride in elements, the columns contiguous.  Rows
+ * aligned to 16 bytes take the wide loads. */
+typedef struct {
+  void* data;
+  int64_t row_stride;
+} evo_matrix;
+
+/* Weights in 4-bit floats (e2m1, as in the fp4 cache) with a scale for each group
+ * of 32 values of a row, a power of two held as its exponent:
+ *   W[n][k] = code[n][k] * 2^(scales[n][k / 32] - 127)       (255: NaN)
+ *   codes   device uint8 [n_out][64 * c], two codes a byte, the lower k in the low half
+ *   scales  device uint8 [n_out][4 * c],  c = ceil(n_in / 128)
+ * Codes and scales of k >= n_in are 0.  codes 16-byte aligned.  (With n_in a multiple
+ * of 128 this is the usual layout of such weights.) */
+typedef struct {
+  const void* codes;
+  const void* scales;
+  int32_t n_out, n_in;
+} evo_weights4;
+
+enum { EVO_ACT_NONE = 0, EVO_ACT_SILU = 1, EVO_ACT_GELU = 2 /* exact erf */ };
+
+/* out = act(x W^T + bias), x [n_rows][n_in], out [n_rows][n_out] of dtype (EVO_FP32
+ * or EVO_BF16), bias device float [n_out] or NULL.  Weights are exact in the
+ * operands of either type; sums, bias and activation are fp32, rounded once.  The
+ * sum of a row has the same bits wherever it stands among the rows of calls with the
+ * same n_rows.  out must not overlap x. */
+int evo_coded_linear(const evo_weights4* w, int32_t dtype, int32_t n_rows, const evo_matrix* x, const float* bias,
+                int32_t activation, const evo_matrix* out, void* hip_stream);
+
+/* Norms after one block and before the next, with the gate and the residual
+ * between them, for every row:
+ *   x' = alpha x + gate * post(y)
+ *   h  = pre(x') * (1 + scale) + shift
+ * where post and pre are one of
+ *   EVO_NORM_RMS    n(u) = u / sqrt(mean(u^2) + eps) * gain + bias
+ *   EVO_NORM_LAYER  n(u) = (u - mean(u)) / sqrt(mean((u - mean(u))^2) + eps) * gain + bias
+ * and EVO_NORM_NONE leaves out the norm of y (post), or h with all that belongs to
+ * it (pre).  Gains are 1, biases, gate's absence and scale's and shift's leave out
+ * their factor or term, where NULL.  Arithmetic is fp32; h is made of the unrounded
+ * x'; each output is rounded once. */
+enum { EVO_NORM_NONE = 0, EVO_NORM_RMS = 1, EVO_NORM_LAYER = 2 };
+typedef struct {
+  int32_t stream_dtype;    /* of x and x_out: EVO_FP32, or the block's */
+  int32_t block_dtype;     /* of y, h, gate, scale and shift */
+  int32_t d;               /* 1 .. 16384 */
+  int32_t post, pre;       /* EVO_NORM_* */
+  float alpha, eps;        /* eps >= 0 */
+  const float* post_gain;  /* device [d] or NULL, these four */
+  const float* post_bias;
+  const float* pre_gain;
+  const float* pre_bias;
+  int32_t n_mods;          /* rows of gate, scale and shift, which have d columns */
+  evo_matrix gate, scale, shift;
+  const int32_t* mod_rows; /* device [n_rows]: which of them a row takes; a number outside them makes the row's
+                              outputs NaN.  NULL: row i takes i / (n_rows / n_mods), n_rows a multiple */
+} evo_block_norm_desc;
+
+/* x, y (NULL: without its term), x_out (NULL: not stored), h: [n_rows][d].  x_out may
+ * be x, and h may be y, with the same strides; no other overlap. */
+int evo_block_norm(const evo_block_norm_desc* desc, int32_t n_rows, const evo_matrix* x, const evo_matrix* y,
+                   const evo_matrix* x_out, const evo_matrix* h, void* hip_stream);
+
 /* Thread-local message of the last failed call on this thread. */
 const char* evo_last_error(void);
 

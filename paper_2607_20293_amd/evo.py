@@ -30,7 +30,8 @@ EXPORTED = ("evo_weight_count", "evo_check_desc", "evo_create_policy", "evo_set_
             "evo_search", "evo_encoder_weight_count", "evo_create_encoder", "evo_encode", "evo_encoder_flops",
             "evo_destroy_encoder", "evo_set_kernel_timing", "evo_kernel_time", "evo_denoise_noalloc",
             "evo_noalloc_scratch_bytes", "evo_debug_encoder_plan", "evo_qk_norm_rope", "evo_cache_write",
-            "evo_cache_read", "evo_qkv_write", "evo_chunk_attention", "evo_chunk_attention_workspace")
+            "evo_cache_read", "evo_qkv_write", "evo_chunk_attention", "evo_chunk_attention_workspace", "evo_coded_linear",
+            "evo_block_norm")
 
 
 def guided_probabilities(scores, eps: float, gamma: float) -> np.ndarray:
@@ -281,6 +282,11 @@ def lib() -> ctypes.CDLL:
         L.evo_chunk_attention_workspace.restype = ctypes.c_int64
         L.evo_chunk_attention.argtypes = [C, R, A, H, H, P, P, ctypes.c_size_t, P]
         L.evo_chunk_attention.restype = ctypes.c_int
+        W, M, B = (ctypes.POINTER(x) for x in (Weights4Desc, Matrix, BlockNormDesc))
+        L.evo_coded_linear.argtypes = [W, I32, I32, M, P, I32, M, P]
+        L.evo_coded_linear.restype = ctypes.c_int
+        L.evo_block_norm.argtypes = [B, I32, M, M, M, M, P]
+        L.evo_block_norm.restype = ctypes.c_int
         L.evo_last_error.argtypes = []
         L.evo_last_error.restype = ctypes.c_char_p
         _lib = L
@@ -980,3 +986,201 @@ def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_ro
         work = space.data_ptr()
     _enqueue(device, L.evo_chunk_attention, desc, rows, att, _heads("q", q, dtype, qs, device), ho, lse_at, work, need)
     return out, lse
+
+
+# --------------------------------------------------------------------------
+# layers around the attention: products with 4-bit weights, norms around a block
+#
+# Streams and gradients as for the operators above.
+# --------------------------------------------------------------------------
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+
+
+class Weights4Desc(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("n_out", ctypes.c_int32),
+                ("n_in", ctypes.c_int32)]
+
+
+class BlockNormDesc(ctypes.Structure):
+    _fields_ = [("stream_dtype", ctypes.c_int32), ("block_dtype", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("alpha", ctypes.c_float), ("eps", ctypes.c_float),
+                ("post_gain", ctypes.c_void_p), ("post_bias", ctypes.c_void_p), ("pre_gain", ctypes.c_void_p),
+                ("pre_bias", ctypes.c_void_p), ("n_mods", ctypes.c_int32), ("gate", Matrix), ("scale", Matrix),
+                ("shift", Matrix), ("mod_rows", ctypes.c_void_p)]
+
+
+ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+_ACTS = {None: ACT_NONE, "silu": ACT_SILU, "gelu": ACT_GELU}
+_NORMS = {None: NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
+
+
+def _matrix(name, t, dtype, shape, device) -> Matrix:
+    """A [rows][columns] tensor with any row stride."""
+    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
+            or (t.requires_grad and torch.is_grad_enabled())):
+        _wrong(name, t, dtype, shape, device)
+    row, one = t.stride()
+    if one != 1 and shape[1] != 1:
+        raise ValueError(f"{name}: its rows must be contiguous")
+    return Matrix(t.data_ptr(), row)
+
+
+class Weights4:
+    """4-bit weights around the caller's tensors (evo_weights4 in include/evo.h):
+    codes [n_out][64 c] (uint8 or float4_e2m1fn_x2) and scales [n_out][4 c] (uint8
+    or float8_e8m0fnu), c = ceil(n_in / 128), zeros behind n_in."""
+
+    def __init__(self, codes, scales, n_in: int):
+        device = _device_of(codes)
+        if codes.dim() != 2 or codes.dtype not in (torch.uint8, torch.float4_e2m1fn_x2):
+            raise TypeError("codes must be [n_out][bytes] of uint8 or float4_e2m1fn_x2")
+        if not isinstance(scales, torch.Tensor) or scales.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+            raise TypeError("scales must be of uint8 or float8_e8m0fnu")
+        n_out, chunks = codes.shape[0], -(-n_in // 128)
+        self.desc = Weights4Desc(_ptr("codes", codes, codes.dtype, (n_out, 64 * chunks), device),
+                                 _ptr("scales", scales, scales.dtype, (n_out, 4 * chunks), device), n_out, n_in)
+        self.codes, self.scales, self.device, self.n_out, self.n_in = codes, scales, device, n_out, n_in
+
+    @staticmethod
+    def coded(w):
+        """(codes, scales) of weights w [n_out][n_in], on w's device: the scale of a
+        group is the least power of two that brings its largest magnitude to 6 or
+        below (2^-126 to 2^125), the codes are the nearest, ties to even.  Weights
+        must be finite."""
+        if w.dim() != 2 or not w.dtype.is_floating_point:
+            raise ValueError("w must be [n_out][n_in] of floats")
+        if not bool(torch.isfinite(w).all()):
+            raise ValueError("weights must be finite")
+        n_out, n_in = w.shape
+        full = w.new_zeros((n_out, -(-n_in // 128) * 128), dtype=torch.float32)
+        full[:, :n_in] = w
+        groups = full.unflatten(1, (-1, 32))
+        top = groups.abs().amax(-1)
+        m, k = torch.frexp(top)                       # top = m 2^k, m in [1/2, 1): top <= 6 2^(k-3) where m <= 3/4
+        e = (k - torch.where(m <= 0.75, 3, 2)).clamp(-126, 125)
+        y = torch.ldexp(groups, -e[..., None])
+        a = y.abs()
+        code = torch.zeros_like(y, dtype=torch.uint8)
+        for border, closed in ((0.25, False), (0.75, True), (1.25, False), (1.75, True), (2.5, False), (3.5, True), (5.0, False)):
+            code += (a >= border) if closed else (a > border)
+        code += (y < 0).to(torch.uint8) * 8
+        code = code.flatten(1)
+        scales = torch.where(top > 0, e + 127, torch.zeros_like(e)).to(torch.uint8)
+        return (code[:, 0::2] | (code[:, 1::2] << 4)).contiguous(), scales.contiguous()
+
+    @classmethod
+    def of(cls, w):
+        """Weights w [n_out][n_in] (a HIP tensor) quantised."""
+        return cls(*cls.coded(w), w.shape[1])
+
+    def values(self):
+        """The weights that the codes stand for, float32 [n_out][n_in]."""
+        b = self.codes.view(torch.uint8)
+        grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=b.device)
+        grid = torch.cat([grid, -grid])
+        v = grid[torch.stack([b & 15, b >> 4], dim=-1).flatten(1).int()]
+        unit = self.scales.view(torch.uint8).to(torch.int32)
+        unit = torch.where(unit == 255, float("nan"), torch.ldexp(torch.ones((), device=b.device), unit - 127))
+        return (v.unflatten(1, (-1, 32)) * unit[..., None]).flatten(1)[:, :self.n_in]
+
+    def tensors(self):
+        return [self.codes, self.scales]
+
+
+def linear4(x, weights: Weights4, bias=None, activation: Optional[str] = None, out=None, stream=None):
+    """evo_coded_linear: act(x W^T + bias) of x [rows][n_in] (float32 or bfloat16, any
+    row stride) with 4-bit weights; bias float32 [n_out] or None; activation None,
+    "silu" or "gelu".  Returns out [rows][n_out] of x's type."""
+    device, dtype = weights.device, x.dtype
+    if stream is not None:
+        return _on_stream(stream, device, (*weights.tensors(), x, bias, out),
+                          lambda: (linear4(x, weights, bias, activation, out),))[0]
+    if activation not in _ACTS:
+        raise ValueError("activation must be None, 'silu' or 'gelu'")
+    dt = _row_dtype(x)
+    if x.dim() != 2:
+        raise ValueError("x must be [rows][n_in]")
+    n, n_out = x.shape[0], weights.n_out
+    xm = _matrix("x", x, dtype, (n, weights.n_in), device)
+    if out is None:
+        out = x.new_empty(n, n_out)
+        om = Matrix(out.data_ptr(), n_out)
+    else:
+        om = _matrix("out", out, dtype, (n, n_out), device)
+    _enqueue(device, lib().evo_coded_linear, weights.desc, dt, n, xm,
+             None if bias is None else _ptr("bias", bias, torch.float32, (n_out,), device), _ACTS[activation], om)
+    return out
+
+
+def block_norm(x, y=None, *, pre: Optional[str] = "rms", post: Optional[str] = None, pre_gain=None, pre_bias=None,
+               post_gain=None, post_bias=None, gate=None, scale=None, shift=None, mod_rows=None, alpha: float = 1.0,
+               eps: float = 1e-6, dtype=None, x_out=None, h_out=None, stream=None):
+    """evo_block_norm: x' = alpha x + gate post(y), h = pre(x') (1 + scale) + shift.
+    x [rows][d] is the residual stream, y the block's output (None: without its
+    term); pre and post are "rms", "layer" or None (post: y as it is; pre: no h);
+    gains and biases float32 [d]; gate, scale and shift [n_mods][d], a row of which
+    belongs to each row of x: mod_rows (int32 [rows]) or, without it, to as many rows
+    each.  dtype: of y, h and the modulation (y's, or x's without y).  x_out may be
+    x, h_out may be y.  Returns (x', h), h None without pre; x' is x itself where
+    there is no y, alpha is 1 and x_out is None."""
+    device = _device_of(x)
+    if stream is not None:
+        def again():
+            return block_norm(x, y, pre=pre, post=post, pre_gain=pre_gain, pre_bias=pre_bias, post_gain=post_gain,
+                              post_bias=post_bias, gate=gate, scale=scale, shift=shift, mod_rows=mod_rows, alpha=alpha, eps=eps,
+                              dtype=dtype, x_out=x_out, h_out=h_out)
+        kept = [None]
+
+        def made():
+            kept[0] = again()
+            return [t for t in kept[0] if t is not None]
+        _on_stream(stream, device, (x, y, pre_gain, pre_bias, post_gain, post_bias, gate, scale, shift, mod_rows, x_out, h_out),
+                   made)
+        return kept[0]
+    if pre not in _NORMS or post not in _NORMS:
+        raise ValueError("pre and post must be 'rms', 'layer' or None")
+    if x.dim() != 2:
+        raise ValueError("x must be [rows][d]")
+    shape = x.shape
+    n, d = shape
+    block = dtype if dtype is not None else x.dtype if y is None else y.dtype
+    xm = _matrix("x", x, x.dtype, shape, device)
+    ym = None if y is None else _matrix("y", y, block, shape, device)
+    desc = BlockNormDesc(_row_dtype(x), {torch.bfloat16: EVO_BF16, torch.float32: EVO_FP32}.get(block, -1), d, _NORMS[post],
+                         _NORMS[pre], alpha, eps)
+    if desc.block_dtype < 0:
+        raise TypeError(f"expected float32 or bfloat16 blocks, got {block}")
+    for name, t in (("post_gain", post_gain), ("post_bias", post_bias), ("pre_gain", pre_gain), ("pre_bias", pre_bias)):
+        if t is not None:
+            setattr(desc, name, _ptr(name, t, torch.float32, (d,), device))
+    mods = None
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if t is not None:
+            if mods is None:
+                mods = t.shape[0]
+            setattr(desc, name, _matrix(name, t, block, (mods, d), device))
+    if mods is not None:
+        desc.n_mods = mods
+    if mod_rows is not None:
+        desc.mod_rows = _ptr("mod_rows", mod_rows, torch.int32, (n,), device)
+    xo = None
+    if x_out is not None:
+        xo = _matrix("x_out", x_out, x.dtype, shape, device)
+    elif y is None and alpha == 1.0:
+        x_out = x
+    else:
+        x_out = x.new_empty(n, d)
+        xo = Matrix(x_out.data_ptr(), d)
+    ho = None
+    if pre is None:
+        if h_out is not None:
+            raise ValueError("h_out without pre's norm")
+    elif h_out is not None:
+        ho = _matrix("h_out", h_out, block, shape, device)
+    else:
+        h_out = x.new_empty(n, d, dtype=block)
+        ho = Matrix(h_out.data_ptr(), d)
+    _enqueue(device, lib().evo_block_norm, desc, n, xm, ym, xo, ho)
+    return x_out, h_out
