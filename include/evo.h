@@ -720,11 +720,12 @@ enum { EVO_ACT_NONE = 0, EVO_ACT_SILU = 1, EVO_ACT_GELU = 2 /* exact erf */ };
 
 /* out = act(x W^T + bias), x [n_rows][n_in], out [n_rows][n_out] of dtype (EVO_FP32
  * or EVO_BF16), bias device float [n_out] or NULL.  Weights are exact in the
- * operands of either type; sums, bias and activation are fp32, rounded once.  The
- * sum of a row has the same bits wherever it stands among the rows of calls with the
- * same n_rows.  out must not overlap x. */
+ * operands of either type; sums, bias and activation are fp32, rounded once.  A
+ * row's result does not depend on the values of other rows; the order of its sum goes by
+ * the sizes of the call and the row's place, so that equal calls give equal bits.  out
+ * must not overlap x. */
 int evo_coded_linear(const evo_weights4* w, int32_t dtype, int32_t n_rows, const evo_matrix* x, const float* bias,
-                int32_t activation, const evo_matrix* out, void* hip_stream);
+                     int32_t activation, const evo_matrix* out, void* hip_stream);
 
 /* Norms after one block and before the next, with the gate and the residual
  * between them, for every row:

@@ -147,7 +147,7 @@ int evo_block_norm(const evo_block_norm_desc* desc, int32_t n_rows, const evo_ma
 }
 
 int evo_coded_linear(const evo_weights4* w, int32_t dtype, int32_t n_rows, const evo_matrix* x, const float* bias,
-                int32_t activation, const evo_matrix* out, void* hip_stream) {
+                     int32_t activation, const evo_matrix* out, void* hip_stream) {
   clear_error();
   if (!w) return fail(EVO_E_INVALID, "weights are NULL");
   TRY(check_dtype("dtype", dtype));
@@ -174,7 +174,6 @@ int evo_coded_linear(const evo_weights4* w, int32_t dtype, int32_t n_rows, const
   a.n_out = w->n_out;
   a.chunks = (w->n_in + 127) / 128;
   a.act = activation;
-  a.wide_x = is_wide(a.x, dtype);
   a.wide_out = is_wide(a.out, dtype);
   return launched(launch_linear4(dtype, compute_units(), a, (hipStream_t)hip_stream));
 }

@@ -35,7 +35,7 @@ struct LinearArgs {
   const float* bias;
   int n_rows, n_in, n_out, chunks;  // chunks: of 128 values of a weight row
   int act;
-  int wide_x, wide_out;             // rows 16-byte aligned
+  int wide_out;                     // rows of out 16-byte aligned
 };
 hipError_t launch_linear4(int dtype, int n_cu, const LinearArgs& a, hipStream_t stream);
 
