@@ -26,6 +26,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "evo.h"
@@ -99,9 +100,15 @@ template <int S> __device__ __forceinline__ uint32_t fp4_bf16(uint32_t v) {
 // instruction wants neighbouring keys of one channel: half bytes are exchanged
 // while they are codes, two operations a channel, which leaves pairs of keys in
 // bytes 0 and 2.
-__device__ __forceinline__ uint32_t select_bits(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
+// (one instruction, which the compiler does not make of these masks: 128 chunks of 32
+// tokens over 1100 positions 38.9 us, else 40.2)
+__device__ __forceinline__ uint32_t select_bits(uint32_t mask, uint32_t a, uint32_t b) {
+  uint32_t x;
+  asm("v_bfi_b32 %0, %1, %2, %3" : "=v"(x) : "s"(mask), "v"(a), "v"(b));
+  return x;
+}
 __device__ __forceinline__ uint32_t even_channel(uint32_t v) { return select_bits(0x000f000fu, v, v >> 4); }
-__device__ __forceinline__ uint32_t odd_channel(uint32_t v) { return even_channel(v >> 4); }
+__device__ __forceinline__ uint32_t odd_channel(uint32_t v) { return select_bits(0x000f000fu, v >> 4, v >> 8); }
 __device__ __forceinline__ u32x2 channel_bf16(uint32_t v) { return u32x2{fp4_bf16<0>(v), fp4_bf16<2>(v)}; }
 // eight codes of fp4 side by side
 __device__ __forceinline__ u32x4 row_bf16(uint32_t v) {
@@ -1615,8 +1622,18 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   const int64_t wgs = (int64_t)p.n_tiles * n_kv_heads;
   // parts of the keys: two workgroups for every compute unit (one of eight
   // waves), each with a few blocks for every wave (part_blocks)
-  const int64_t want = wgs ? ((p.tile_rows == 256 ? 1 : 2) * (int64_t)n_cu + wgs - 1) / wgs : 1;
-  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, blocks / part_blocks(wgs, n_cu)));
+  int64_t each = p.tile_rows == 256 ? 1 : 2, most = blocks / part_blocks(wgs, n_cu);
+  // Over fp4, where a block's bytes are a quarter and a part's join weighs more: three,
+  // and no more parts than a part has blocks (one token over 65536 positions, 8 heads of
+  // 128, 27.0 us with 64 parts, 22.0 with 32; 12 heads of 64 over 16384 16.6 with 42,
+  // 11.4 with 16; 6 ragged sequences of up to 65001 65 with two, 54 with three, 59 with
+  // four; 6 equally long ones 113, 90 and 104).
+  if (format == EVO_CACHE_FP4 && p.tile_rows <= 32) {
+    each = 3;
+    most = std::min(most, (int64_t)std::ceil(std::sqrt((double)blocks)));
+  }
+  const int64_t want = wgs ? (each * n_cu + wgs - 1) / wgs : 1;
+  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(want, most));
   // a workgroup that has its compute unit to itself brings eight waves, unless its
   // part has fewer blocks than that
   p.waves = wgs * p.n_split <= n_cu && (p.n_split == 1 || blocks / p.n_split >= 8) && eight_waves(format, head_dim, p.tile_rows) ? 8 : kWaves;

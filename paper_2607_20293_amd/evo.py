@@ -282,10 +282,10 @@ def lib() -> ctypes.CDLL:
         L.evo_chunk_attention_workspace.restype = ctypes.c_int64
         L.evo_chunk_attention.argtypes = [C, R, A, H, H, P, P, ctypes.c_size_t, P]
         L.evo_chunk_attention.restype = ctypes.c_int
-        W, M, B = (ctypes.POINTER(x) for x in (Weights4Desc, Matrix, BlockNormDesc))
+        W, M = (ctypes.POINTER(x) for x in (Weights4Desc, Matrix))
         L.evo_coded_linear.argtypes = [W, I32, I32, M, P, I32, M, P]
         L.evo_coded_linear.restype = ctypes.c_int
-        L.evo_block_norm.argtypes = [B, I32, M, M, M, M, P]
+        L.evo_block_norm.argtypes = [P, I32, M, M, M, M, P]  # (a BlockNormDesc's address)
         L.evo_block_norm.restype = ctypes.c_int
         L.evo_last_error.argtypes = []
         L.evo_last_error.restype = ctypes.c_char_p
@@ -1010,21 +1010,33 @@ class BlockNormDesc(ctypes.Structure):
                 ("shift", Matrix), ("mod_rows", ctypes.c_void_p)]
 
 
+class _FlatNormDesc(ctypes.Structure):
+    """BlockNormDesc with its matrices field by field: one structure is made faster than four."""
+    _fields_ = [f for name, kind in BlockNormDesc._fields_
+                for f in ([(name, ctypes.c_void_p), (name + "_row", ctypes.c_int64)] if kind is Matrix else [(name, kind)])]
+
+
 ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 _ACTS = {None: ACT_NONE, "silu": ACT_SILU, "gelu": ACT_GELU}
 _NORMS = {None: NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
+_NORM_TYPES = {torch.bfloat16: EVO_BF16, torch.float32: EVO_FP32}
+_NOWHERE = (None, 0)
 
 
-def _matrix(name, t, dtype, shape, device) -> Matrix:
-    """A [rows][columns] tensor with any row stride."""
+def _rows_at(name, t, dtype, shape, device):
+    """Address and row stride of a [rows][columns] tensor."""
     if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
             or (t.requires_grad and torch.is_grad_enabled())):
         _wrong(name, t, dtype, shape, device)
     row, one = t.stride()
     if one != 1 and shape[1] != 1:
         raise ValueError(f"{name}: its rows must be contiguous")
-    return Matrix(t.data_ptr(), row)
+    return t.data_ptr(), row
+
+
+def _matrix(name, t, dtype, shape, device) -> Matrix:
+    return Matrix(*_rows_at(name, t, dtype, shape, device))
 
 
 class Weights4:
@@ -1146,25 +1158,26 @@ def block_norm(x, y=None, *, pre: Optional[str] = "rms", post: Optional[str] = N
     shape = x.shape
     n, d = shape
     block = dtype if dtype is not None else x.dtype if y is None else y.dtype
+    if block not in _NORM_TYPES:
+        raise TypeError(f"expected float32 or bfloat16 blocks, got {block}")
     xm = _matrix("x", x, x.dtype, shape, device)
     ym = None if y is None else _matrix("y", y, block, shape, device)
-    desc = BlockNormDesc(_row_dtype(x), {torch.bfloat16: EVO_BF16, torch.float32: EVO_FP32}.get(block, -1), d, _NORMS[post],
-                         _NORMS[pre], alpha, eps)
-    if desc.block_dtype < 0:
-        raise TypeError(f"expected float32 or bfloat16 blocks, got {block}")
-    for name, t in (("post_gain", post_gain), ("post_bias", post_bias), ("pre_gain", pre_gain), ("pre_bias", pre_bias)):
-        if t is not None:
-            setattr(desc, name, _ptr(name, t, torch.float32, (d,), device))
-    mods = None
-    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
-        if t is not None:
-            if mods is None:
-                mods = t.shape[0]
-            setattr(desc, name, _matrix(name, t, block, (mods, d), device))
-    if mods is not None:
-        desc.n_mods = mods
-    if mod_rows is not None:
-        desc.mod_rows = _ptr("mod_rows", mod_rows, torch.int32, (n,), device)
+    f32, mods, gate_at, scale_at, shift_at = torch.float32, 0, _NOWHERE, _NOWHERE, _NOWHERE
+    if gate is not None or scale is not None or shift is not None:
+        mods = (gate if gate is not None else scale if scale is not None else shift).shape[0]
+        if gate is not None:
+            gate_at = _rows_at("gate", gate, block, (mods, d), device)
+        if scale is not None:
+            scale_at = _rows_at("scale", scale, block, (mods, d), device)
+        if shift is not None:
+            shift_at = _rows_at("shift", shift, block, (mods, d), device)
+    desc = _FlatNormDesc(_row_dtype(x), _NORM_TYPES[block], d, _NORMS[post], _NORMS[pre], alpha, eps,
+                         None if post_gain is None else _ptr("post_gain", post_gain, f32, (d,), device),
+                         None if post_bias is None else _ptr("post_bias", post_bias, f32, (d,), device),
+                         None if pre_gain is None else _ptr("pre_gain", pre_gain, f32, (d,), device),
+                         None if pre_bias is None else _ptr("pre_bias", pre_bias, f32, (d,), device),
+                         mods, *gate_at, *scale_at, *shift_at,
+                         None if mod_rows is None else _ptr("mod_rows", mod_rows, torch.int32, (n,), device))
     xo = None
     if x_out is not None:
         xo = _matrix("x_out", x_out, x.dtype, shape, device)
@@ -1182,5 +1195,5 @@ def block_norm(x, y=None, *, pre: Optional[str] = "rms", post: Optional[str] = N
     else:
         h_out = x.new_empty(n, d, dtype=block)
         ho = Matrix(h_out.data_ptr(), d)
-    _enqueue(device, lib().evo_block_norm, desc, n, xm, ym, xo, ho)
+    _enqueue(device, lib().evo_block_norm, ctypes.byref(desc), n, xm, ym, xo, ho)
     return x_out, h_out
