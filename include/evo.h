@@ -755,8 +755,8 @@ typedef struct {
                               outputs NaN.  NULL: row i takes i / (n_rows / n_mods), n_rows a multiple */
 } evo_block_norm_desc;
 
-/* x, y (NULL: without its term), x_out (NULL: not stored), h: [n_rows][d].  x_out may
- * be x, and h may be y, with the same strides; no other overlap. */
+/* x, y (NULL: without its term), x_out (NULL: not stored), h: [n_rows][d], up to 2^24 - 1
+ * rows (2^23 - 1 where d is above 2048, 2^22 - 1 above 4096).  x_out may be x, and h may be y, with the same strides; no other overlap. */
 int evo_block_norm(const evo_block_norm_desc* desc, int32_t n_rows, const evo_matrix* x, const evo_matrix* y,
                    const evo_matrix* x_out, const evo_matrix* h, void* hip_stream);
 

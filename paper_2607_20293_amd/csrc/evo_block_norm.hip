@@ -1,10 +1,15 @@
 // Norms after a block and before the next, with the block's gate and the residual
 // between them, in one pass over the rows (evo_block_norm).
 //
-// A row lies over LPR lanes (a part of a wave, a wave, or a workgroup's four), 8
-// values a lane and chunk, and stays in registers from its load to its stores: sums
-// of squares, and for layer norms sums first, are lane exchanges (and four words
-// of LDS where four waves share a row).
+// A row lies over LPR lanes (a part of a wave, a wave, or up to 16 of them), 8 values
+// a lane and chunk, and stays in registers from its load to its stores: sums
+// of squares, and for layer norms sums first, are lane exchanges (and a word of LDS for
+// each wave where several share a row).
+//
+// What bounds it: memory (65537 rows of 1024, fp32 stream and bf16 blocks, each with its
+// modulation: 148 us, 5.4 TB/s, where a copy has 4.92), latencies for few rows (16 rows of
+// 256: 4.3 us in a recorded graph; requesting gains and modulation with the row saved 5%
+// and cost wide rows their registers).
 #include <hip/hip_runtime.h>
 
 #include "evo.h"
@@ -14,6 +19,7 @@ namespace evo {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kFewRows = 1500;
 
 // 8 values from index `at` of a row of d; those behind its end are `fill`
 template <bool WIDE> __device__ __forceinline__ void load8(const float* p, int at, int d, float fill, float* x) {
@@ -71,15 +77,25 @@ template <bool WIDE> __device__ __forceinline__ void store8(__bf16* p, int at, i
   }
 }
 
-// The row's sum over its lanes.  `sums`: four words that no other sum of the
-// workgroup uses.
+// threads of a workgroup whose rows take so many lanes
+constexpr int threads_of(int lpr) { return lpr > kThreads ? lpr : kThreads; }
+
+// The row's sum over its lanes.  `sums`: a word for each of its waves that no other
+// sum of the workgroup uses.
 template <int LPR> __device__ __forceinline__ float row_sum(float x, float* sums) {
 #pragma unroll
   for (int s = 1; s < (LPR < 64 ? LPR : 64); s *= 2) x += __shfl_xor(x, s);
   if constexpr (LPR > 64) {
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = x;
     __syncthreads();
-    x = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    float y[LPR / 64];
+#pragma unroll
+    for (int w = 0; w < LPR / 64; ++w) y[w] = sums[w];
+#pragma unroll
+    for (int n = LPR / 128; n >= 1; n /= 2)
+#pragma unroll
+      for (int w = 0; w < n; ++w) y[w] = y[2 * w] + y[2 * w + 1];
+    x = y[0];
   }
   return x;
 }
@@ -104,7 +120,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& a, int kind, const floa
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int e = 0; e < 8; ++e) s = fmaf(x[c][e], x[c][e], s);
-  const float r = 1.f / sqrtf(fmaf(row_sum<LPR>(s, sums + 4), a.inv_d, a.eps));
+  const float r = 1.f / sqrtf(fmaf(row_sum<LPR>(s, sums + (LPR > 64 ? LPR / 64 : 0)), a.inv_d, a.eps));
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     float g[8], b[8];
@@ -120,10 +136,10 @@ __device__ __forceinline__ void norm_row(const NormArgs& a, int kind, const floa
 }
 
 template <typename TS, typename TB, int LPR, int C, bool WIDE>
-__global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
-  __shared__ float sums[LPR > 64 ? 16 : 1];
+__global__ void __launch_bounds__(threads_of(LPR)) norm_kernel(NormArgs a) {
+  __shared__ float sums[LPR > 64 ? LPR / 16 : 1];
   const int lane = threadIdx.x % LPR;
-  const int64_t at_row = (int64_t)blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
+  const int64_t at_row = (int64_t)blockIdx.x * (threads_of(LPR) / LPR) + threadIdx.x / LPR;
   // whole waves stay for the exchanges; rows past the end repeat the last one
   // and are not stored
   const bool live = at_row < a.n_rows;
@@ -170,7 +186,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
     for (int c = 0; c < C; ++c) store8<WIDE>(reinterpret_cast<TS*>(a.x_out.p) + n * a.x_out.row, (c * LPR + lane) * 8, a.d, x[c]);
   }
   if (!a.pre) return;
-  norm_row<LPR, C, WIDE>(a, a.pre, a.pre_gain, a.pre_bias, lane, x, sums + (LPR > 64 ? 8 : 0));
+  norm_row<LPR, C, WIDE>(a, a.pre, a.pre_gain, a.pre_bias, lane, x, sums + (LPR > 64 ? LPR / 32 : 0));
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     float m[8], t[8];
@@ -187,22 +203,27 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
 
 template <typename TS, typename TB, int LPR, int C>
 hipError_t launch_as(bool wide, const NormArgs& a, hipStream_t stream) {
-  constexpr int rows = kThreads / LPR;
+  constexpr int rows = threads_of(LPR) / LPR;
   const dim3 grid((unsigned)(((int64_t)a.n_rows + rows - 1) / rows));
-  hipLaunchKernelGGL((wide ? norm_kernel<TS, TB, LPR, C, true> : norm_kernel<TS, TB, LPR, C, false>), grid, dim3(kThreads), 0,
+  hipLaunchKernelGGL((wide ? norm_kernel<TS, TB, LPR, C, true> : norm_kernel<TS, TB, LPR, C, false>), grid, dim3(threads_of(LPR)), 0,
                      stream, a);
   return hipGetLastError();
 }
 
+// Lanes of a row, and 8 values each so many times: as few values a lane as a workgroup
+// allows (8000 rows of 8192, bf16, 134 us over 1024 lanes, 183 over 256; of 16384 318 and
+// 782; 301 rows of 5120 7.4 and 8.3; one row of 8192 5.8 and 8.8).  At 1024 values two a
+// lane spare the exchange between waves, which pays where rows fill the device (3000 rows
+// 9.3 us, else 11.2; 1500 7.1 and 7.2; 300 6.2 and 4.9).
 template <typename TS, typename TB> hipError_t launch_types(bool wide, const NormArgs& a, hipStream_t stream) {
   if (a.d <= 128) return launch_as<TS, TB, 16, 1>(wide, a, stream);
   if (a.d <= 256) return launch_as<TS, TB, 32, 1>(wide, a, stream);
   if (a.d <= 512) return launch_as<TS, TB, 64, 1>(wide, a, stream);
-  if (a.d <= 1024) return launch_as<TS, TB, 64, 2>(wide, a, stream);
+  if (a.d <= 1024 && a.n_rows > kFewRows) return launch_as<TS, TB, 64, 2>(wide, a, stream);
   if (a.d <= 2048) return launch_as<TS, TB, 256, 1>(wide, a, stream);
-  if (a.d <= 4096) return launch_as<TS, TB, 256, 2>(wide, a, stream);
-  if (a.d <= 8192) return launch_as<TS, TB, 256, 4>(wide, a, stream);
-  return launch_as<TS, TB, 256, 8>(wide, a, stream);
+  if (a.d <= 4096) return launch_as<TS, TB, 512, 1>(wide, a, stream);
+  if (a.d <= 8192) return launch_as<TS, TB, 1024, 1>(wide, a, stream);
+  return launch_as<TS, TB, 1024, 2>(wide, a, stream);
 }
 
 }  // namespace

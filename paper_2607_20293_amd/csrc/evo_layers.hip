@@ -12,7 +12,9 @@ namespace evo {
 namespace {
 
 constexpr int kMaxWidth = 16384;         // of a normalised row
-constexpr int kMaxNormRows = (1 << 24) - 1;  // a workgroup's 256 threads each, of 2^32 that a launch may have
+// Rows of a norm: up to 256, 512 or 1024 threads each, of fewer than 2^32 that a launch
+// may have.
+constexpr int max_norm_rows(int d) { return (1 << (d <= 2048 ? 24 : d <= 4096 ? 23 : 22)) - 1; }
 constexpr int kMaxFeatures = 1 << 20;    // rows and columns of weights
 constexpr int kMaxLinearRows = 1 << 20;
 
@@ -93,7 +95,8 @@ int evo_block_norm(const evo_block_norm_desc* desc, int32_t n_rows, const evo_ma
   clear_error();
   TRY(check_norm(desc));
   if (n_rows < 0) return fail(EVO_E_INVALID, "%d rows", n_rows);
-  if (n_rows > kMaxNormRows) return fail(EVO_E_UNSUPPORTED, "%d rows: up to 2^24 - 1", n_rows);
+  if (n_rows > max_norm_rows(desc->d))
+    return fail(EVO_E_UNSUPPORTED, "%d rows of %d: up to %d (2^24 - 1 up to 2048, 2^23 - 1 up to 4096, 2^22 - 1)", n_rows, desc->d, max_norm_rows(desc->d));
   const evo_block_norm_desc& n = *desc;
   if (!y && (n.post || n.gate.data)) return fail(EVO_E_INVALID, "post's norm or a gate without y");
   if (!n.pre != !h) return fail(EVO_E_INVALID, n.pre ? "h is NULL" : "h without pre's norm");

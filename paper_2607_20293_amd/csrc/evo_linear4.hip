@@ -57,7 +57,7 @@ template <typename T> __device__ __forceinline__ u32x4 load_last(const T* row, i
   return v;
 }
 
-// Activations of results that are rounded to T.  In bf16 (half a step: 2^-9 of the
+// Activations of results that are rounded to T.  In bf16 (half a step: 2^-8 of the
 // value) they come from the hardware's exponential and reciprocal, and the normal
 // distribution's tail, 1/2 erfc(z), z = |x| / sqrt(2), from exp(-z^2) t P(t), t = 1 / (1 +
 // 0.44 z), P a least-squares fit of degree 5 to the scaled complement over z to 10.5:

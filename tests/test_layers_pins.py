@@ -222,3 +222,13 @@ def test_weights_values_and_host_tensors():
     w.codes, w.scales, w.n_in = codes, scales, 150
     assert np.array_equal(w.values().double().numpy(), E.weights4(codes.numpy(), scales.numpy(), 150))
     assert float((w.values() - m).abs().max()) <= float(m.abs().max()) / 3
+
+
+def test_block_norm_rows_of_a_launch():
+    """A launch has fewer than 2^32 threads, up to 1024 for a row."""
+    L = _lib()
+    plain = dict(gate=evo.Matrix(), scale=evo.Matrix(), shift=evo.Matrix())
+    wide = _matrix(row_stride=16384)
+    for d, n in ((2049, 1 << 23), (4096, 1 << 23), (4097, 1 << 22), (16384, 1 << 22)):
+        assert _norm(L, n=n, d=d, x=wide, y=wide, x_out=wide, h=wide, **plain) == UNSUPPORTED
+        assert f"up to {n - 1}" in L.evo_last_error().decode()
