@@ -241,11 +241,12 @@ __global__ void __launch_bounds__(64 * WW * WR * KS, WW * WR * KS / 4) tile_kern
   typedef Tile<T, CW, RW, WW, WR, KS> L;
   typedef Step<T> P;
   constexpr int ST = P::kSteps, TH = 64 * WW * WR * KS;
-  static_assert(L::NX % TH == 0, "");
+  static_assert(L::NX % TH == 0 && TH % (KS * L::RC) == 0, "every thread has the same piece of its rows");
   constexpr int IX = L::NX / TH, IW = (L::NW + TH - 1) / TH, IS = (L::NS + TH - 1) / TH;
   __shared__ __attribute__((aligned(16))) char lds[L::kLds];
   // A die takes neighbouring tiles (workgroup i runs on die i % 8), kBand of the rows by
-  // as many of the weights as it holds at a time, so that its cache serves both.
+  // as many of the weights as it holds at a time, so that its cache serves both (4096
+  // rows of 8192 to 8192 features 446 us, with all rows first 463).
   const int per = (int)gridDim.x / 8, tile = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
   if (tile >= tiles) return;
   const int weight_tiles = tiles / row_tiles, band = tile / (kBand * weight_tiles), in_band = tile - band * (kBand * weight_tiles);
@@ -422,23 +423,24 @@ __global__ void __launch_bounds__(64 * WW * WR * KS, WW * WR * KS / 4) tile_kern
             sums[((w - WW * WR) * M + (c * RW + r) * 4 + q) * 64 + lane] = f32x4{o[c][r][4 * q], o[c][r][4 * q + 1], o[c][r][4 * q + 2], o[c][r][4 * q + 3]};
     }
     __syncthreads();
-    if (group == 0)
+    if (group == 0) {
 #pragma unroll
-    for (int g = 0; g < KS - 1; ++g)
+      for (int g = 0; g < KS - 1; ++g)
 #pragma unroll
-      for (int c = 0; c < CW; ++c)
+        for (int c = 0; c < CW; ++c)
 #pragma unroll
-        for (int r = 0; r < RW; ++r)
+          for (int r = 0; r < RW; ++r)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x4 v = sums[((g * WW * WR + w) * M + (c * RW + r) * 4 + q) * 64 + lane];
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 v = sums[((g * WW * WR + w) * M + (c * RW + r) * 4 + q) * 64 + lane];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[c][r][4 * q + e] += v[e];
-          }
+              for (int e = 0; e < 4; ++e) o[c][r][4 * q + e] += v[e];
+            }
+    }
   }
   // results through LDS, so that a row's lie side by side as they are stored
   constexpr int kPitch = L::W * (int)sizeof(T) + 16, kPieces = L::W * (int)sizeof(T) / 16, V = 16 / (int)sizeof(T);
-  static_assert(L::R * kPitch <= L::kLds && TH % kPieces == 0, "");
+  static_assert(L::R * kPitch <= L::kLds && TH % kPieces == 0, "the results fit");
   __syncthreads();
   if (group == 0) {
 #pragma unroll
@@ -535,7 +537,7 @@ template <typename T> const Shape* cheapest(int64_t rows, const LinearArgs& a, i
 
 template <typename T> hipError_t launch_as(const LinearArgs& a, int n_cu, hipStream_t stream) {
   // Rows that fill whole rounds may go before the rest, in a launch of their own:
-  // 2049 rows of 4096 to 4096 features in tiles of 128 by 256 alone 109 us, split 71.
+  // 2049 rows of 4096 to 4096 features in tiles of 128 by 256 alone 109 us, split 75.
   float least;
   const Shape* rest = cheapest<T>(a.n_rows, a, n_cu, &least);
   const Shape* first = nullptr;

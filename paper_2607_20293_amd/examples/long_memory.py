@@ -8,10 +8,13 @@ chunk alone: its tokens lie behind the memory, write their keys and values over
 the step before's, and attend to memory and chunk.  A layer's two residuals are
 computed where the lattice says so and added from their cache elsewhere (Eq. 1).
 
+With weights in 4 bits the products are `evo.linear4`'s, and `evo.block_norm` adds a
+residual and normalises what the next block reads in one pass.
+
 The steps of a chunk are recorded once into a HIP graph and replayed for every
 set of queries of the same lattice.
 
-    python -m paper_2607_20293_amd.examples.long_memory [--queries 16] [--memory 2000] [--format int8]
+    python -m paper_2607_20293_amd.examples.long_memory [--queries 16] [--memory 2000] [--format int8] [--weights 4bit]
 
 prints one JSON line.  Weights and inputs are synthetic.
 """
@@ -25,7 +28,8 @@ import torch
 from paper_2607_20293_amd import evo
 
 DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
-FORMATS = {"fp32": torch.float32, "bf16": torch.bfloat16, "int8": torch.int8, "fp8": torch.float8_e4m3fn}
+FORMATS = {"fp32": torch.float32, "bf16": torch.bfloat16, "int8": torch.int8, "fp8": torch.float8_e4m3fn,
+           "fp4": torch.float4_e2m1fn_x2}
 EPS = 1e-6
 
 
@@ -34,7 +38,7 @@ class MemoryPolicy:
     caches of `lengths` memories (tokens of each query)."""
 
     def __init__(self, lengths, chunk=16, layers=4, heads=4, kv_heads=4, dh=64, ff=1024, dtype="bf16", fmt="bf16", seed=0,
-                 page=64, device="cuda"):
+                 page=64, device="cuda", weights=None):
         self.lengths, self.chunk, self.layers = list(lengths), chunk, layers
         self.heads, self.kv_heads, self.dh, self.d = heads, kv_heads, dh, heads * dh
         self.dtype, self.device = DTYPES[dtype], torch.device(device, torch.cuda.current_device())
@@ -47,6 +51,14 @@ class MemoryPolicy:
         self.out = [weight(heads * dh, self.d) for _ in range(layers)]
         self.up = [weight(self.d, ff) for _ in range(layers)]
         self.down = [weight(ff, self.d) for _ in range(layers)]
+        if weights not in (None, "4bit"):
+            raise ValueError("weights must be None (the dtype's) or '4bit'")
+        self.coded = None
+        if weights:
+            self.coded = {}
+            for name in ("qkv", "out", "up", "down"):
+                self.coded[name] = [evo.Weights4.of(w.t().contiguous()) for w in getattr(self, name)]
+                setattr(self, name, [c.values().t() for c in self.coded[name]])  # what the codes stand for
         self.gains = [tuple((1 + 0.1 * torch.randn(dh, generator=g)).to(self.device) for _ in range(2)) for _ in range(layers)]
 
         n = len(self.lengths)
@@ -74,25 +86,42 @@ class MemoryPolicy:
         f = x.float()
         return (f * torch.rsqrt((f * f).mean(-1, keepdim=True) + EPS)).to(x.dtype)
 
-    def _attention(self, layer, x, starts, lengths, cu, most, causal):
-        """The attention's residual of tokens x [rows][d]."""
+    def _product(self, name, layer, x, activation=None):
+        if self.coded:
+            return evo.linear4(x, self.coded[name][layer], activation=activation)
+        y = x @ getattr(self, name)[layer]
+        return torch.nn.functional.silu(y) if activation else y
+
+    def _normed(self, x):
+        return evo.block_norm(x, eps=EPS)[1] if self.coded else self._norm(x)
+
+    def _add(self, x, residual, normed):
+        """x + residual and, where the next block reads it, its norm."""
+        if self.coded:
+            return evo.block_norm(x, residual, pre="rms" if normed else None, eps=EPS)
+        x = x + residual
+        return x, self._norm(x) if normed else None
+
+    def _attention(self, layer, x, starts, lengths, cu, most, causal, h=None):
+        """The attention's residual of tokens x [rows][d] (h: their norm, where
+        it is there)."""
         hq, hk = self.heads, self.kv_heads
-        y = (self._norm(x) @ self.qkv[layer]).unflatten(1, (hq + 2 * hk, self.dh))
+        y = self._product("qkv", layer, self._normed(x) if h is None else h).unflatten(1, (hq + 2 * hk, self.dh))
         cache = self.caches[layer]
         q = evo.qkv_write(cache, self.table, starts, y[:, :hq], y[:, hq:hq + hk], y[:, hq + hk:], self.rope,
                           *self.gains[layer], EPS, "halves", cu, most)
         a, _ = evo.chunk_attention(q, cache, self.table, lengths, cu, most, causal=causal)
-        return a.flatten(1) @ self.out[layer]
+        return self._product("out", layer, a.flatten(1))
 
-    def _forward(self, layer, x):
-        return torch.nn.functional.silu(self._norm(x) @ self.up[layer]) @ self.down[layer]
+    def _forward(self, layer, h):
+        return self._product("down", layer, self._product("up", layer, h, "silu"))
 
     def write_memory(self, tokens):
         """tokens [sum of lengths][d], the queries' memories one after another."""
-        x = tokens
+        x, h = tokens, None
         for i in range(self.layers):
-            x = x + self._attention(i, x, self.zero, self.held, self.cu, max(self.lengths), True)
-            x = x + self._forward(i, x)
+            x, h = self._add(x, self._attention(i, x, self.zero, self.held, self.cu, max(self.lengths), True, h), True)
+            x, h = self._add(x, self._forward(i, h), i + 1 < self.layers)
 
     def denoise(self, noise, lattice):
         """noise [steps + 1][queries][chunk][d]: the first is the chunk the
@@ -102,14 +131,14 @@ class MemoryPolicy:
         held = [[None, None] for _ in range(self.layers)]
         steps = noise.shape[0] - 1
         for t in range(steps):
-            y = x
+            y, h = x, None
             for i in range(self.layers):
                 if lattice[i][t]:
-                    held[i][0] = self._attention(i, y, self.held, self.total, None, None, False)
-                y = y + held[i][0]
+                    held[i][0] = self._attention(i, y, self.held, self.total, None, None, False, h)
+                y, h = self._add(y, held[i][0], lattice[i][t])
                 if lattice[i][t]:
-                    held[i][1] = self._forward(i, y)
-                y = y + held[i][1]
+                    held[i][1] = self._forward(i, h)
+                y, h = self._add(y, held[i][1], i + 1 < self.layers and lattice[i + 1][t])
             keep = 0.9
             x = keep * x + (1 - keep) * y + 0.1 * noise[t + 1].flatten(0, 1)
         return x.unflatten(0, (len(self.lengths), self.chunk))
@@ -140,11 +169,12 @@ def main(argv=None):
     p.add_argument("--every", type=int, default=4, help="refresh every so many steps")
     p.add_argument("--dtype", choices=sorted(DTYPES), default="bf16")
     p.add_argument("--format", choices=sorted(FORMATS), default=None, help="of the cache (default: the dtype)")
+    p.add_argument("--weights", choices=["4bit"], default=None, help="held in 4 bits (default: in the dtype)")
     a = p.parse_args(argv)
     if a.queries < 1 or a.memory < 1 or a.steps < 1 or a.every < 1:
         p.error("queries, memory, steps and every are at least 1")
     lengths = [max(1, a.memory - a.memory * s // (2 * a.queries)) for s in range(a.queries)]
-    pol = MemoryPolicy(lengths, dtype=a.dtype, fmt=a.format or a.dtype)
+    pol = MemoryPolicy(lengths, dtype=a.dtype, fmt=a.format or a.dtype, weights=a.weights)
     g = torch.Generator(device=pol.device).manual_seed(1)
     tokens = torch.randn((sum(lengths), pol.d), generator=g, device=pol.device).to(pol.dtype)
     noise = torch.randn((a.steps + 1, a.queries, pol.chunk, pol.d), generator=g, device=pol.device).to(pol.dtype)
@@ -158,7 +188,8 @@ def main(argv=None):
     graph.replay()
     marks[2].record()
     torch.cuda.synchronize()
-    print(json.dumps({"queries": a.queries, "memory_tokens": sum(lengths), "cache": a.format or a.dtype, "steps": a.steps,
+    print(json.dumps({"queries": a.queries, "memory_tokens": sum(lengths), "cache": a.format or a.dtype,
+                      "weights": a.weights or a.dtype, "steps": a.steps,
                       "refreshed_steps": sum(lattice[0]), "finite": bool(torch.isfinite(out).all()),
                       "write_memory_ms": round(marks[0].elapsed_time(marks[1]), 3),
                       "denoise_ms": round(marks[1].elapsed_time(marks[2]), 3)}), flush=True)
