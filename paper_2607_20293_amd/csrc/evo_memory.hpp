@@ -127,6 +127,7 @@ struct AttArgs {
 struct AttPlan {
   int tile_rows, tiles_per_seq, n_tiles, n_split, waves;
   int64_t part_floats, ml_floats, flags;
+  bool rest;  // terms of 16 significant bits
 };
 
 AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_kv_heads, const RowsView& r,

@@ -409,6 +409,7 @@ __device__ __forceinline__ f32x4 score_tile(const uint32_t* k, const Query<float
 template <typename T> struct Terms;
 template <> struct Terms<__bf16> {
   bf16x8 f[2];
+  __device__ __forceinline__ float at(int t, int i) const { return (float)f[t / 2][t % 2 * 4 + i]; }
   __device__ __forceinline__ void set(const float (&p)[4][4]) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -420,6 +421,7 @@ template <> struct Terms<__bf16> {
 };
 template <> struct Terms<float> {
   float f[4][4];
+  __device__ __forceinline__ float at(int t, int i) const { return f[t][i]; }
   __device__ __forceinline__ void set(const float (&p)[4][4]) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -458,18 +460,27 @@ __device__ __forceinline__ f32x4 value_tile(const uint32_t* v, const Terms<float
   return o;
 }
 
-// The same for the two tiles of a tile of fp4 value rows.
-__device__ __forceinline__ void value_tiles(const uint32_t* v, const Terms<__bf16>& p, f32x4* o) {
+// The same for the two tiles of a tile of fp4 value rows.  REST: also for what the
+// terms' rounding left.
+template <bool REST>
+__device__ __forceinline__ void value_tiles(const uint32_t* v, const Terms<__bf16>& p, const Terms<__bf16>& rest, f32x4* o) {
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     const uint32_t a = v[2 * s], b = v[2 * s + 1];
     const u32x2 e0 = channel_bf16(even_channel(a)), e1 = channel_bf16(even_channel(b));
     const u32x2 d0 = channel_bf16(odd_channel(a)), d1 = channel_bf16(odd_channel(b));
-    o[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{e0[0], e0[1], e1[0], e1[1]}), p.f[s], o[0], 0, 0, 0);
-    o[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{d0[0], d0[1], d1[0], d1[1]}), p.f[s], o[1], 0, 0, 0);
+    const bf16x8 e = __builtin_bit_cast(bf16x8, u32x4{e0[0], e0[1], e1[0], e1[1]});
+    const bf16x8 d = __builtin_bit_cast(bf16x8, u32x4{d0[0], d0[1], d1[0], d1[1]});
+    o[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e, p.f[s], o[0], 0, 0, 0);
+    o[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d, p.f[s], o[1], 0, 0, 0);
+    if constexpr (REST) {
+      o[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e, rest.f[s], o[0], 0, 0, 0);
+      o[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d, rest.f[s], o[1], 0, 0, 0);
+    }
   }
 }
-__device__ __forceinline__ void value_tiles(const uint32_t* v, const Terms<float>& p, f32x4* o) {
+template <bool REST>
+__device__ __forceinline__ void value_tiles(const uint32_t* v, const Terms<float>& p, const Terms<float>&, f32x4* o) {
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -671,7 +682,12 @@ template <typename T> constexpr int waves_per_simd(int f, int dh, int r, int nw)
 // PARTS: the keys are split over workgroups (of its own, because the join's
 // code costs the others registers: 32-token chunks over fp8 memories 47 us with
 // it and 45 without).
-template <typename T, int F, int DH, int R, int NW, bool PARTS>
+// REST (bf16 over fp4, the smallest calls): what the terms' rounding to bf16 leaves is
+// the operand of a second product.  Where few keys carry a row, the rounded value scale of
+// one is the error of all its outputs: one token over 1000 positions was up to 0.0030 off
+// without it, 0.0018 with it as a result rounded once (7.5 us, else 7.4).  Larger calls pay for it in their vector units and
+// registers (128 single tokens over 2000 38 us, else 34).
+template <typename T, int F, int DH, int R, int NW, bool PARTS, bool REST = false>
 __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stream_kernel(AttArgs a) {
   typedef Lay<F, DH> L;
   constexpr int TR = 16 * R;
@@ -825,7 +841,7 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
     }
     __builtin_amdgcn_sched_barrier(0);
 
-    Terms<T> terms[R];
+    Terms<T> terms[R], rests[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float x[4][4];
@@ -881,6 +897,10 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
         if (masked) each([&](float& x, int t, int i) { x = seen.at(kb + L::key_of(t, g, i)) ? x : 0.f; });
       }
       terms[r].set(x);
+      if constexpr (REST) {
+        each([&](float& x, int t, int i) { x -= terms[r].at(t, i); });
+        rests[r].set(x);
+      }
     }
     bool bad = false;
     if constexpr (holds_nan(F)) {
@@ -895,7 +915,7 @@ __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stre
     for (int c = 0; c < L::VT; ++c)
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        if constexpr (F == EVO_CACHE_FP4) value_tiles(vr[c], terms[r], &o[r][2 * c]);
+        if constexpr (F == EVO_CACHE_FP4) value_tiles<REST>(vr[c], terms[r], rests[r], &o[r][2 * c]);
         else o[r][c] = value_tile<F>(vr[c], terms[r], o[r][c]);
       }
     if constexpr (holds_nan(F)) {
@@ -1538,7 +1558,14 @@ constexpr int64_t lds_rows(int f, int dh) {
 }
 
 template <typename T, int F, int DH, int R, int NW>
-void launch_stream(int64_t wgs, const AttArgs& a, hipStream_t stream) {
+void launch_stream(int64_t wgs, const AttPlan& p, const AttArgs& a, hipStream_t stream) {
+  if constexpr (F == EVO_CACHE_FP4 && sizeof(T) == 2 && R == 1 && NW > 1) {
+    if (p.rest) {
+      hipLaunchKernelGGL((a.n_split > 1 ? stream_kernel<T, F, DH, R, NW, true, true> : stream_kernel<T, F, DH, R, NW, false, true>),
+                         dim3(wgs), dim3(NW * 64), 0, stream, a);
+      return;
+    }
+  }
   if constexpr (NW == 1)  // (not in parts)
     hipLaunchKernelGGL((stream_kernel<T, F, DH, R, 1, false>), dim3(wgs), dim3(64), 0, stream, a);
   else if constexpr (NW == 4 || eight_waves(F, DH, 16 * R))
@@ -1553,13 +1580,13 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
   if (p.tiles_per_seq > 1) wgs = (wgs / p.tiles_per_seq + 7) / 8 * 8 * p.tiles_per_seq;  // (see find_unit)
   constexpr int R2 = two_row_blocks(F, DH) ? 2 : 1;
   if (p.tile_rows == 16) {
-    if (p.waves == 1) launch_stream<T, F, DH, 1, 1>(wgs, a, stream);
-    else if (p.waves == 8) launch_stream<T, F, DH, 1, 8>(wgs, a, stream);
-    else launch_stream<T, F, DH, 1, 4>(wgs, a, stream);
+    if (p.waves == 1) launch_stream<T, F, DH, 1, 1>(wgs, p, a, stream);
+    else if (p.waves == 8) launch_stream<T, F, DH, 1, 8>(wgs, p, a, stream);
+    else launch_stream<T, F, DH, 1, 4>(wgs, p, a, stream);
   } else if (p.tile_rows == 32) {
-    if (p.waves == 1) launch_stream<T, F, DH, R2, 1>(wgs, a, stream);
-    else if (p.waves == 8) launch_stream<T, F, DH, R2, 8>(wgs, a, stream);
-    else launch_stream<T, F, DH, R2, 4>(wgs, a, stream);
+    if (p.waves == 1) launch_stream<T, F, DH, R2, 1>(wgs, p, a, stream);
+    else if (p.waves == 8) launch_stream<T, F, DH, R2, 8>(wgs, p, a, stream);
+    else launch_stream<T, F, DH, R2, 4>(wgs, p, a, stream);
   } else if constexpr (sizeof(T) == 2 && lds_rows(F, DH) != kNever) {
     const bool far = a.cap > kFastCap;
     if (p.tile_rows == 128)
@@ -1642,6 +1669,7 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   // over 27 positions 491 us with four waves and 129 with one, int8 136 and 48;
   // over 250 93 and 52, int8 27 and 20; over 1000 126 and 111, int8 35 and 43)
   if (p.tile_rows <= 32 && p.n_split == 1 && wgs >= 4 * (int64_t)n_cu && blocks <= 8) p.waves = 1;
+  p.rest = dtype == EVO_BF16 && format == EVO_CACHE_FP4 && rows <= 8 && p.waves > 1 && wgs * p.n_split <= n_cu;
   if (p.n_split > 1) {
     p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
     p.part_floats = wgs * p.n_split * p.tile_rows * head_dim;
