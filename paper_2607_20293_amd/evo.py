@@ -1165,6 +1165,8 @@ def block_norm(x, y=None, *, pre: Optional[str] = "rms", post: Optional[str] = N
     f32, mods, gate_at, scale_at, shift_at = torch.float32, 0, _NOWHERE, _NOWHERE, _NOWHERE
     if gate is not None or scale is not None or shift is not None:
         mods = (gate if gate is not None else scale if scale is not None else shift).shape[0]
+        if n and not mods:
+            raise ValueError("gate, scale and shift have no rows")
         if gate is not None:
             gate_at = _rows_at("gate", gate, block, (mods, d), device)
         if scale is not None:

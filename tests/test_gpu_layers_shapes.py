@@ -95,3 +95,16 @@ def test_block_norm_widths(stream, block, rows, d):
     for pre, post in (("rms", "layer"), ("layer", "rms")):
         call = NormCall(device(), stream, block, rows, d, pre=pre, post=post, mods=1, seed=d)
         call.check(f"{rows} x {d}, {pre} after {post}")
+
+
+def test_block_norm_of_no_rows():
+    """No rows give none; a modulation of none for some rows is refused."""
+    dev = device()
+    x, none = torch.randn((4, 64), device=dev), torch.empty((0, 64), device=dev)
+    for kw in (dict(y=x, gate=none), dict(scale=none), dict(shift=none)):
+        with pytest.raises(ValueError):
+            evo.block_norm(x, **kw)
+    out, h = evo.block_norm(none, none, gate=x[:1], scale=x[:1])
+    assert out.shape == h.shape == (0, 64)
+    w = random_weights(16, 64, torch.Generator().manual_seed(1), dev)
+    assert evo.linear4(none, w).shape == (0, 16)
