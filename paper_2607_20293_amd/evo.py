@@ -1060,14 +1060,14 @@ class Weights4:
         """(codes, scales) of weights w [n_out][n_in], on w's device: the scale of a
         group is the least power of two that brings its largest magnitude to 6 or
         below (2^-126 to 2^125), the codes are the nearest, ties to even.  Weights
-        must be finite."""
+        must be finite floats of 32 bits."""
         if w.dim() != 2 or not w.dtype.is_floating_point:
             raise ValueError("w must be [n_out][n_in] of floats")
-        if not bool(torch.isfinite(w).all()):
-            raise ValueError("weights must be finite")
         n_out, n_in = w.shape
         full = w.new_zeros((n_out, -(-n_in // 128) * 128), dtype=torch.float32)
         full[:, :n_in] = w
+        if not bool(torch.isfinite(full).all()):
+            raise ValueError("weights must be finite in 32 bits")
         groups = full.unflatten(1, (-1, 32))
         top = groups.abs().amax(-1)
         m, k = torch.frexp(top)                       # top = m 2^k, m in [1/2, 1): top <= 6 2^(k-3) where m <= 3/4
