@@ -707,6 +707,7 @@ typedef struct {
 /* Weights in 4-bit floats (e2m1, as in the fp4 cache) with a scale for each group
  * of 32 values of a row, a power of two held as its exponent:
  *   W[n][k] = code[n][k] * 2^(scales[n][k / 32] - 127)       (255: NaN)
+ * (a weight of 2^128 or more is an infinity of its sign)
  *   codes   device uint8 [n_out][64 * c], two codes a byte, the lower k in the low half
  *   scales  device uint8 [n_out][4 * c],  c = ceil(n_in / 128)
  * Codes and scales of k >= n_in are 0.  codes 16-byte aligned.  (With n_in a multiple
