@@ -729,6 +729,13 @@ enum { EVO_ACT_NONE = 0, EVO_ACT_SILU = 1, EVO_ACT_GELU = 2 /* exact erf */ };
 int evo_coded_linear(const evo_weights4* w, int32_t dtype, int32_t n_rows, const evo_matrix* x, const float* bias,
                      int32_t activation, const evo_matrix* out, void* hip_stream);
 
+/* Test query: how evo_coded_linear would run a call of these sizes on a device of
+ * n_cu compute units.  out [11] receives the number of kernels that the dtype has and,
+ * for each launch in order: which of them (from 0), the launch's rows, rows and weight
+ * rows of a tile, parts of K in a workgroup.  Returns the number of launches (1 or 2),
+ * or a negative EVO_E_* code.  Host-only. */
+int evo_debug_linear_plan(int32_t dtype, int32_t n_rows, int32_t n_in, int32_t n_out, int32_t n_cu, int32_t* out);
+
 /* Norms after one block and before the next, with the gate and the residual
  * between them, for every row:
  *   x' = alpha x + gate * post(y)

@@ -75,6 +75,23 @@ int check_norm(const evo_block_norm_desc* n) {
   return EVO_OK;
 }
 
+int check_linear_sizes(int dtype, int n_rows, int n_in, int n_out) {
+  TRY(check_dtype("dtype", dtype));
+  if (n_out < 1 || n_in < 1) return fail(EVO_E_INVALID, "weights of %d by %d", n_out, n_in);
+  if (n_out > kMaxFeatures || n_in > kMaxFeatures)
+    return fail(EVO_E_UNSUPPORTED, "weights of %d by %d: up to 2^20 each", n_out, n_in);
+  if (n_rows < 0) return fail(EVO_E_INVALID, "%d rows", n_rows);
+  if (n_rows > kMaxLinearRows) return fail(EVO_E_UNSUPPORTED, "%d rows: up to 2^20", n_rows);
+  return EVO_OK;
+}
+
+void set_linear_sizes(LinearArgs* a, int n_rows, int n_in, int n_out) {
+  a->n_rows = n_rows;
+  a->n_in = n_in;
+  a->n_out = n_out;
+  a->chunks = (n_in + 127) / 128;
+}
+
 // Compute units of the current device (see evo_memory.hip's).
 int compute_units() {
   int dev = 0, n = 0;
@@ -153,14 +170,9 @@ int evo_coded_linear(const evo_weights4* w, int32_t dtype, int32_t n_rows, const
                      int32_t activation, const evo_matrix* out, void* hip_stream) {
   clear_error();
   if (!w) return fail(EVO_E_INVALID, "weights are NULL");
-  TRY(check_dtype("dtype", dtype));
-  if (w->n_out < 1 || w->n_in < 1) return fail(EVO_E_INVALID, "weights of %d by %d", w->n_out, w->n_in);
-  if (w->n_out > kMaxFeatures || w->n_in > kMaxFeatures)
-    return fail(EVO_E_UNSUPPORTED, "weights of %d by %d: up to 2^20 each", w->n_out, w->n_in);
+  TRY(check_linear_sizes(dtype, n_rows, w->n_in, w->n_out));
   if (!w->codes || !w->scales) return fail(EVO_E_INVALID, "codes or scales are NULL");
   if (!aligned(w->codes, 16)) return fail(EVO_E_INVALID, "codes must be 16-byte aligned");
-  if (n_rows < 0) return fail(EVO_E_INVALID, "%d rows", n_rows);
-  if (n_rows > kMaxLinearRows) return fail(EVO_E_UNSUPPORTED, "%d rows: up to 2^20", n_rows);
   if (activation < EVO_ACT_NONE || activation > EVO_ACT_GELU) return fail(EVO_E_INVALID, "bad activation %d", activation);
   TRY(check_floats("bias", bias));
   if (!n_rows) return EVO_OK;
@@ -172,13 +184,19 @@ int evo_coded_linear(const evo_weights4* w, int32_t dtype, int32_t n_rows, const
   a.x = view(x);
   a.out = view(out);
   a.bias = bias;
-  a.n_rows = n_rows;
-  a.n_in = w->n_in;
-  a.n_out = w->n_out;
-  a.chunks = (w->n_in + 127) / 128;
+  set_linear_sizes(&a, n_rows, w->n_in, w->n_out);
   a.act = activation;
   a.wide_out = is_wide(a.out, dtype);
   return launched(launch_linear4(dtype, compute_units(), a, (hipStream_t)hip_stream));
+}
+
+int evo_debug_linear_plan(int32_t dtype, int32_t n_rows, int32_t n_in, int32_t n_out, int32_t n_cu, int32_t* out) {
+  clear_error();
+  TRY(check_linear_sizes(dtype, n_rows, n_in, n_out));
+  if (n_rows < 1 || n_cu < 1 || !out) return fail(EVO_E_INVALID, "bad argument");
+  LinearArgs a = {};
+  set_linear_sizes(&a, n_rows, n_in, n_out);
+  return describe_linear4(dtype, n_cu, a, out);
 }
 
 }  // extern "C"

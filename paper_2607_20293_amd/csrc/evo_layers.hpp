@@ -38,5 +38,7 @@ struct LinearArgs {
   int wide_out;                     // rows of out 16-byte aligned
 };
 hipError_t launch_linear4(int dtype, int n_cu, const LinearArgs& a, hipStream_t stream);
+// Its launches, as evo_debug_linear_plan tells them.
+int describe_linear4(int dtype, int n_cu, const LinearArgs& a, int32_t* out);
 
 }  // namespace evo

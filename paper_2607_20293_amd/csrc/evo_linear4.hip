@@ -493,26 +493,26 @@ template <typename T, int C> void launch_few(const LinearArgs& a, hipStream_t st
 // the order below, 1000 rows 330, 223, 85, 69, 51, 46 and 51, 4000 rows 1307, 872, 316,
 // 242, 192, 171 and 131.
 struct Shape {
-  int rows, weights;
+  int rows, weights, parts;  // parts: of K in a workgroup
   float start, chunk;
   float least;  // what a round of one tile takes of that; 0: a compute unit holds several workgroups
   void (*launch)(const LinearArgs&, hipStream_t);
 };
 template <typename T> struct Shapes;
 template <> struct Shapes<__bf16> {
-  static constexpr Shape of[] = {{16, 16, 0.02f, 0.168f, 0.f, launch_few<__bf16, 1>},
-                                 {16, 32, 0.05f, 0.225f, 0.f, launch_few<__bf16, 2>},
-                                 {32, 64, 4.6f, 0.18f, 0.95f, launch_tiles<__bf16, 1, 1, 2, 1, 4>},
-                                 {32, 128, 3.2f, 0.375f, 0.88f, launch_tiles<__bf16, 1, 1, 4, 1, 2>},
-                                 {64, 128, 4.8f, 0.595f, 0.8f, launch_tiles<__bf16, 2, 1, 2, 2, 2>},
-                                 {128, 128, 4.f, 1.16f, 0.65f, launch_tiles<__bf16, 1, 2, 4, 2, 1>},
-                                 {128, 256, 10.f, 1.7f, 0.68f, launch_tiles<__bf16, 2, 2, 4, 2, 1>}};
+  static constexpr Shape of[] = {{16, 16, 8, 0.02f, 0.168f, 0.f, launch_few<__bf16, 1>},
+                                 {16, 32, 8, 0.05f, 0.225f, 0.f, launch_few<__bf16, 2>},
+                                 {32, 64, 4, 4.6f, 0.18f, 0.95f, launch_tiles<__bf16, 1, 1, 2, 1, 4>},
+                                 {32, 128, 2, 3.2f, 0.375f, 0.88f, launch_tiles<__bf16, 1, 1, 4, 1, 2>},
+                                 {64, 128, 2, 4.8f, 0.595f, 0.8f, launch_tiles<__bf16, 2, 1, 2, 2, 2>},
+                                 {128, 128, 1, 4.f, 1.16f, 0.65f, launch_tiles<__bf16, 1, 2, 4, 2, 1>},
+                                 {128, 256, 1, 10.f, 1.7f, 0.68f, launch_tiles<__bf16, 2, 2, 4, 2, 1>}};
 };
 template <> struct Shapes<float> {
-  static constexpr Shape of[] = {{16, 16, 0.05f, 0.36f, 0.f, launch_few<float, 1>},
-                                 {16, 32, 0.3f, 0.375f, 0.f, launch_few<float, 2>},
-                                 {32, 128, 5.f, 2.15f, 0.97f, launch_tiles<float, 1, 1, 4, 1, 2>},
-                                 {64, 256, 6.f, 7.85f, 0.97f, launch_tiles<float, 2, 1, 4, 2, 1>}};
+  static constexpr Shape of[] = {{16, 16, 8, 0.05f, 0.36f, 0.f, launch_few<float, 1>},
+                                 {16, 32, 8, 0.3f, 0.375f, 0.f, launch_few<float, 2>},
+                                 {32, 128, 2, 5.f, 2.15f, 0.97f, launch_tiles<float, 1, 1, 4, 1, 2>},
+                                 {64, 256, 1, 6.f, 7.85f, 0.97f, launch_tiles<float, 2, 1, 4, 2, 1>}};
 };
 constexpr float kLaunch = 2.f;
 float cost(const Shape& s, int64_t rows, const LinearArgs& a, int n_cu) {
@@ -535,13 +535,17 @@ template <typename T> const Shape* cheapest(int64_t rows, const LinearArgs& a, i
   return best;
 }
 
-template <typename T> hipError_t launch_as(const LinearArgs& a, int n_cu, hipStream_t stream) {
+// The launches of a call: `rest` takes what `first` (or NULL) leaves.
+struct Launches {
+  const Shape* first;
+  int first_rows;
+  const Shape* rest;
+};
+template <typename T> Launches plan(const LinearArgs& a, int n_cu) {
   // Rows that fill whole rounds may go before the rest, in a launch of their own:
   // 2049 rows of 4096 to 4096 features in tiles of 128 by 256 alone 109 us, split 75.
   float least;
-  const Shape* rest = cheapest<T>(a.n_rows, a, n_cu, &least);
-  const Shape* first = nullptr;
-  int first_rows = 0;
+  Launches p = {nullptr, 0, cheapest<T>(a.n_rows, a, n_cu, &least)};
   for (const Shape& s : Shapes<T>::of) {
     if (s.least == 0.f) continue;
     const int64_t wt = (a.n_out + s.weights - 1) / s.weights, rt = a.n_rows / s.rows;
@@ -551,28 +555,51 @@ template <typename T> hipError_t launch_as(const LinearArgs& a, int n_cu, hipStr
       float c;
       const Shape* other = cheapest<T>(a.n_rows - rows, a, n_cu, &c);
       c += cost(s, rows, a, n_cu);
-      if (c < least) { least = c; first = &s; first_rows = (int)rows; rest = other; }
+      if (c < least) { least = c; p = {&s, (int)rows, other}; }
     }
   }
+  return p;
+}
+
+template <typename T> hipError_t launch_as(const LinearArgs& a, int n_cu, hipStream_t stream) {
+  const Launches p = plan<T>(a, n_cu);
   LinearArgs b = a;
-  if (first) {
-    b.n_rows = first_rows;
-    first->launch(b, stream);
+  if (p.first) {
+    b.n_rows = p.first_rows;
+    p.first->launch(b, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     b = a;
-    b.n_rows -= first_rows;
-    b.x.p += first_rows * b.x.row * (int64_t)sizeof(T);
-    b.out.p += first_rows * b.out.row * (int64_t)sizeof(T);
+    b.n_rows -= p.first_rows;
+    b.x.p += p.first_rows * b.x.row * (int64_t)sizeof(T);
+    b.out.p += p.first_rows * b.out.row * (int64_t)sizeof(T);
   }
-  rest->launch(b, stream);
+  p.rest->launch(b, stream);
   return hipGetLastError();
+}
+
+template <typename T> int describe_as(const LinearArgs& a, int n_cu, int32_t* out) {
+  const Launches p = plan<T>(a, n_cu);
+  constexpr int kinds = sizeof(Shapes<T>::of) / sizeof(Shape);
+  *out++ = kinds;
+  int n = 0;
+  const auto add = [&](const Shape* s, int rows) {
+    for (int v : {(int)(s - Shapes<T>::of), rows, s->rows, s->weights, s->parts}) *out++ = v;
+    ++n;
+  };
+  if (p.first) add(p.first, p.first_rows);
+  add(p.rest, a.n_rows - p.first_rows);
+  return n;
 }
 
 }  // namespace
 
 hipError_t launch_linear4(int dtype, int n_cu, const LinearArgs& a, hipStream_t stream) {
   return dtype == EVO_BF16 ? launch_as<__bf16>(a, n_cu, stream) : launch_as<float>(a, n_cu, stream);
+}
+
+int describe_linear4(int dtype, int n_cu, const LinearArgs& a, int32_t* out) {
+  return dtype == EVO_BF16 ? describe_as<__bf16>(a, n_cu, out) : describe_as<float>(a, n_cu, out);
 }
 
 }  // namespace evo

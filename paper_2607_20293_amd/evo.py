@@ -31,7 +31,7 @@ EXPORTED = ("evo_weight_count", "evo_check_desc", "evo_create_policy", "evo_set_
             "evo_destroy_encoder", "evo_set_kernel_timing", "evo_kernel_time", "evo_denoise_noalloc",
             "evo_noalloc_scratch_bytes", "evo_debug_encoder_plan", "evo_qk_norm_rope", "evo_cache_write",
             "evo_cache_read", "evo_qkv_write", "evo_chunk_attention", "evo_chunk_attention_workspace", "evo_coded_linear",
-            "evo_block_norm")
+            "evo_debug_linear_plan", "evo_block_norm")
 
 
 def guided_probabilities(scores, eps: float, gamma: float) -> np.ndarray:
@@ -285,6 +285,8 @@ def lib() -> ctypes.CDLL:
         W, M = (ctypes.POINTER(x) for x in (Weights4Desc, Matrix))
         L.evo_coded_linear.argtypes = [W, I32, I32, M, P, I32, M, P]
         L.evo_coded_linear.restype = ctypes.c_int
+        L.evo_debug_linear_plan.argtypes = [I32, I32, I32, I32, I32, P]
+        L.evo_debug_linear_plan.restype = ctypes.c_int
         L.evo_block_norm.argtypes = [P, I32, M, M, M, M, P]  # (a BlockNormDesc's address)
         L.evo_block_norm.restype = ctypes.c_int
         L.evo_last_error.argtypes = []
@@ -1124,6 +1126,17 @@ def linear4(x, weights: Weights4, bias=None, activation: Optional[str] = None, o
     _enqueue(device, lib().evo_coded_linear, weights.desc, dt, n, xm,
              None if bias is None else _ptr("bias", bias, torch.float32, (n_out,), device), _ACTS[activation], om)
     return out
+
+
+def linear_plan(dtype, n_rows: int, n_in: int, n_out: int, n_cu: int = 256):
+    """How linear4 would run a call of these sizes (host only): (number of kernels of
+    the dtype, int32 [launches][5] of which of them, the launch's rows, rows and weight
+    rows of a tile, parts of K in a workgroup)."""
+    out = np.zeros(11, np.int32)
+    rc = lib().evo_debug_linear_plan(_NORM_TYPES[dtype], n_rows, n_in, n_out, n_cu, out.ctypes.data)
+    if rc < 0:
+        _check(rc)
+    return int(out[0]), out[1:1 + 5 * rc].reshape(rc, 5)
 
 
 def block_norm(x, y=None, *, pre: Optional[str] = "rms", post: Optional[str] = None, pre_gain=None, pre_bias=None,
