@@ -9,10 +9,12 @@ from __future__ import annotations
 import ctypes
 import os
 import sys
+import types
 from typing import Optional, Sequence
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libevo.so")
 
@@ -623,7 +625,8 @@ class Encoder:
 # wait for, and what has to wait for it, is the caller's to say.
 #
 # These are inference operators: none has a gradient.  A tensor that requires one
-# is refused while gradients are recorded, instead of its gradient being lost.
+# is refused while gradients are recorded, and one with a tangent of forward mode,
+# instead of its gradient being lost.
 # --------------------------------------------------------------------------
 class KVCacheDesc(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
@@ -665,6 +668,14 @@ def _row_dtype(t) -> int:
     raise TypeError(f"expected float32 or bfloat16 rows, got {t.dtype}")
 
 
+# (torch counts dual levels, of forward mode, from 0: outside of them nothing has a tangent)
+_levels = forward_ad if hasattr(forward_ad, "_current_level") else types.SimpleNamespace(_current_level=0)
+
+
+def _has_tangent(t) -> bool:
+    return forward_ad.unpack_dual(t).tangent is not None
+
+
 # The checks below run at every call of operators that take a few microseconds:
 # one comparison of everything, the reason looked for only where it fails;
 # nothing checked of tensors made here; sizes as numbers and structures as they
@@ -672,6 +683,8 @@ def _row_dtype(t) -> int:
 def _wrong(name, t, dtype, shape, device):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a tensor")
+    if _has_tangent(t):
+        raise RuntimeError(f"{name} has a tangent, and this operator has no forward mode: call it with detached tensors")
     if t.requires_grad and torch.is_grad_enabled():
         raise RuntimeError(f"{name} requires a gradient, and this operator has none: call it under torch.no_grad(), or "
                            "with detached tensors")
@@ -685,7 +698,8 @@ def _wrong(name, t, dtype, shape, device):
 def _heads(name, t, dtype, shape, device) -> Heads:
     """A [rows][heads][dh] tensor with any row and head strides."""
     if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
-            or (t.requires_grad and torch.is_grad_enabled())):
+            or (t.requires_grad and torch.is_grad_enabled())
+            or (_levels._current_level >= 0 and _has_tangent(t))):
         _wrong(name, t, dtype, shape, device)
     row, head, one = t.stride()
     if one != 1:
@@ -701,7 +715,8 @@ def _new(like, rows, heads, dh):
 
 def _ptr(name, t, dtype, shape, device) -> int:
     if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
-            or not t.is_contiguous() or (t.requires_grad and torch.is_grad_enabled())):
+            or not t.is_contiguous() or (t.requires_grad and torch.is_grad_enabled())
+            or (_levels._current_level >= 0 and _has_tangent(t))):
         _wrong(name, t, dtype, shape, device)
     return t.data_ptr()
 
@@ -1029,7 +1044,8 @@ _NOWHERE = (None, 0)
 def _rows_at(name, t, dtype, shape, device):
     """Address and row stride of a [rows][columns] tensor."""
     if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape
-            or (t.requires_grad and torch.is_grad_enabled())):
+            or (t.requires_grad and torch.is_grad_enabled())
+            or (_levels._current_level >= 0 and _has_tangent(t))):
         _wrong(name, t, dtype, shape, device)
     row, one = t.stride()
     if one != 1 and shape[1] != 1:
