@@ -868,7 +868,7 @@ def qk_norm_rope(q, k, positions, table, q_gain=None, k_gain=None, eps: Optional
     k_out), which may be (q, k).  Returns (q_out, k_out)."""
     device = _device_of(q)
     if stream is not None:
-        return _on_stream(stream, device, (q, k, positions, table, q_gain, k_gain),
+        return _on_stream(stream, device, (q, k, positions, table, q_gain, k_gain, *(out or ())),
                           lambda: qk_norm_rope(q, k, positions, table, q_gain, k_gain, eps, pairs, out))
     dt, dtype = _row_dtype(q), q.dtype
     if q.dim() != 3 or k.dim() != 3:
@@ -910,7 +910,7 @@ def cache_read(cache: KVCache, page_table, starts, n_rows: int, dtype, cu_rows=N
     [n_rows][kv_heads][dh] of dtype."""
     device, shape = cache.device, (n_rows, cache.n_kv_heads, cache.head_dim)
     if stream is not None:
-        return _on_stream(stream, device, (*cache.tensors(), page_table, starts, cu_rows),
+        return _on_stream(stream, device, (*cache.tensors(), page_table, starts, cu_rows, *(out or ())),
                           lambda: cache_read(cache, page_table, starts, n_rows, dtype, cu_rows, max_rows, out))
     rows = cache.rows(page_table, n_rows, cu_rows, max_rows)
     if out is None:
@@ -932,7 +932,7 @@ def qkv_write(cache: KVCache, page_table, starts, q, k, v, table, q_gain=None, k
     starts[s] + i that are written."""
     device, dh, dtype = cache.device, cache.head_dim, q.dtype
     if stream is not None:
-        return _on_stream(stream, device, (*cache.tensors(), page_table, starts, q, k, v, table, q_gain, k_gain, cu_rows),
+        return _on_stream(stream, device, (*cache.tensors(), page_table, starts, q, k, v, table, q_gain, k_gain, cu_rows, q_out),
                           lambda: (qkv_write(cache, page_table, starts, q, k, v, table, q_gain, k_gain, eps, pairs, cu_rows,
                                              max_rows, q_out),))[0]
     dt = _row_dtype(q)
@@ -968,7 +968,7 @@ def chunk_attention(q, cache: KVCache, page_table, lengths, cu_rows=None, max_ro
                                    window=window, cap=cap, slopes=slopes, prefix=prefix, starts=starts,
                                    max_length=max_length, out=out, lse=lse)
         if stream is not None:
-            return _on_stream(stream, device, (*cache.tensors(), q, page_table, lengths, cu_rows, slopes, prefix, starts),
+            return _on_stream(stream, device, (*cache.tensors(), q, page_table, lengths, cu_rows, slopes, prefix, starts, out, lse),
                               again)
         with torch.cuda.device(device):
             return again()
