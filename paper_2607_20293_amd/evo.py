@@ -658,6 +658,8 @@ class Attention(ctypes.Structure):
 
 CACHE_FP32, CACHE_BF16, CACHE_INT8, CACHE_FP8, CACHE_FP4 = 0, 1, 2, 3, 5
 _PAIRS = {"halves": 0, "adjacent": 1}
+# torch's 4-bit floats and power-of-two scales, None where it has none
+_FP4, _E8M0 = (getattr(torch, name, None) for name in ("float4_e2m1fn_x2", "float8_e8m0fnu"))
 
 
 def _row_dtype(t) -> int:
@@ -790,7 +792,7 @@ class KVCache:
     def __init__(self, k, v, k_scale=None, v_scale=None):
         device = _device_of(k)
         formats = {torch.float32: CACHE_FP32, torch.bfloat16: CACHE_BF16, torch.int8: CACHE_INT8,
-                   torch.float8_e4m3fn: CACHE_FP8, torch.float4_e2m1fn_x2: CACHE_FP4}
+                   torch.float8_e4m3fn: CACHE_FP8, _FP4: CACHE_FP4}
         if k.dtype not in formats:
             raise TypeError(f"no cache format holds {k.dtype}")
         if k.dim() != 4:
@@ -811,12 +813,12 @@ class KVCache:
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 64, dtype=None, device="cuda"):
         """An unwritten cache of its own tensors (dtype: bfloat16 by default)."""
         dtype = torch.bfloat16 if dtype is None else dtype
-        if dtype == torch.float4_e2m1fn_x2 and head_dim % 2:
+        if dtype == _FP4 and head_dim % 2:
             raise ValueError(f"head_dim {head_dim} is not whole elements of {dtype}")
-        wide = head_dim // 2 if dtype == torch.float4_e2m1fn_x2 else head_dim
+        wide = head_dim // 2 if dtype == _FP4 else head_dim
         k = torch.empty((n_pages, n_kv_heads, page_size, wide), dtype=dtype, device=device)
         v = torch.empty((n_pages, n_kv_heads, wide, page_size), dtype=dtype, device=device)
-        if dtype not in (torch.int8, torch.float8_e4m3fn, torch.float4_e2m1fn_x2):
+        if dtype not in (torch.int8, torch.float8_e4m3fn, _FP4):
             return cls(k, v)
         return cls(k, v, *(torch.empty((n_pages, n_kv_heads, page_size), device=device) for _ in range(2)))
 
@@ -1064,9 +1066,9 @@ class Weights4:
 
     def __init__(self, codes, scales, n_in: int):
         device = _device_of(codes)
-        if codes.dim() != 2 or codes.dtype not in (torch.uint8, torch.float4_e2m1fn_x2):
+        if codes.dim() != 2 or codes.dtype not in (torch.uint8, _FP4):
             raise TypeError("codes must be [n_out][bytes] of uint8 or float4_e2m1fn_x2")
-        if not isinstance(scales, torch.Tensor) or scales.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+        if not isinstance(scales, torch.Tensor) or scales.dtype not in (torch.uint8, _E8M0):
             raise TypeError("scales must be of uint8 or float8_e8m0fnu")
         n_out, chunks = codes.shape[0], -(-n_in // 128)
         self.desc = Weights4Desc(_ptr("codes", codes, codes.dtype, (n_out, 64 * chunks), device),

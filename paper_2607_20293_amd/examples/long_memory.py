@@ -28,8 +28,9 @@ import torch
 from paper_2607_20293_amd import evo
 
 DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
-FORMATS = {"fp32": torch.float32, "bf16": torch.bfloat16, "int8": torch.int8, "fp8": torch.float8_e4m3fn,
-           "fp4": torch.float4_e2m1fn_x2}
+FORMATS = {"fp32": torch.float32, "bf16": torch.bfloat16, "int8": torch.int8, "fp8": torch.float8_e4m3fn}
+if hasattr(torch, "float4_e2m1fn_x2"):
+    FORMATS["fp4"] = torch.float4_e2m1fn_x2
 EPS = 1e-6
 
 
