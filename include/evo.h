@@ -659,7 +659,8 @@ int evo_qkv_write(const evo_kv_cache* cache, const evo_kv_rows* rows, const evo_
  * and sums are fp32; with EVO_BF16 the products take bf16 operands (8-bit
  * and 4-bit codes are exact in bf16; the softmax's terms, over such caches with the
  * value's scale in them, are rounded to bf16 for the second product, twice bf16's bits of
- * them in calls over 4-bit caches of few rows that do not fill the device), with
+ * them in calls over 4-bit caches with up to 8 rows of a sequence to a key/value head, or
+ * with max_length (or the page table) of up to 64 positions), with
  * EVO_FP32 fp32 operands.  A capped score is off by a few roundings of itself
  * whatever the cap; with EVO_BF16 and caps up to 64 by up to 2^-22 of the cap
  * instead.  The weighted values are summed before they are

@@ -682,11 +682,15 @@ template <typename T> constexpr int waves_per_simd(int f, int dh, int r, int nw)
 // PARTS: the keys are split over workgroups (of its own, because the join's
 // code costs the others registers: 32-token chunks over fp8 memories 47 us with
 // it and 45 without).
-// REST (bf16 over fp4, the smallest calls): what the terms' rounding to bf16 leaves is
-// the operand of a second product.  Where few keys carry a row, the rounded value scale of
-// one is the error of all its outputs: one token over 1000 positions was up to 0.0030 off
-// without it, 0.0018 with it as a result rounded once (7.5 us, else 7.4).  Larger calls pay for it in their vector units and
-// registers (128 single tokens over 2000 38 us, else 34).
+// REST (bf16 over fp4): what the terms' rounding to bf16 leaves is the operand of a
+// second product.  Where few keys carry a row, the rounded value scale of one is the error
+// of all its outputs: up to 0.0030 without it, 0.0017 with it as a result rounded once.  It
+// goes by the rows and positions of a sequence, so that a row's bits do not go by how many
+// others share its call: single tokens (one over 1000 positions 7.5 us, else 7.4; 6 over up to
+// 65001 54.0, else 52.4; 128 over 2000 38, else 34), and a block of keys for any rows
+// (1600 rows of 84 sequences over 27 positions 130 us with and without).  Other
+// calls would pay for it in their vector units (128 chunks of 32 over up to 1100 42.5 us, so
+// 38.6; 2000 causal rows of 8 sequences 100, so 91), and are 0.0024 off.
 template <typename T, int F, int DH, int R, int NW, bool PARTS, bool REST = false>
 __global__ void __launch_bounds__(NW * 64, waves_per_simd<T>(F, DH, R, NW)) stream_kernel(AttArgs a) {
   typedef Lay<F, DH> L;
@@ -1559,10 +1563,13 @@ constexpr int64_t lds_rows(int f, int dh) {
 
 template <typename T, int F, int DH, int R, int NW>
 void launch_stream(int64_t wgs, const AttPlan& p, const AttArgs& a, hipStream_t stream) {
-  if constexpr (F == EVO_CACHE_FP4 && sizeof(T) == 2 && R == 1 && NW > 1) {
+  if constexpr (F == EVO_CACHE_FP4 && sizeof(T) == 2 && R == 1) {
     if (p.rest) {
-      hipLaunchKernelGGL((a.n_split > 1 ? stream_kernel<T, F, DH, R, NW, true, true> : stream_kernel<T, F, DH, R, NW, false, true>),
-                         dim3(wgs), dim3(NW * 64), 0, stream, a);
+      if constexpr (NW == 1)
+        hipLaunchKernelGGL((stream_kernel<T, F, DH, R, 1, false, true>), dim3(wgs), dim3(64), 0, stream, a);
+      else
+        hipLaunchKernelGGL((a.n_split > 1 ? stream_kernel<T, F, DH, R, NW, true, true> : stream_kernel<T, F, DH, R, NW, false, true>),
+                           dim3(wgs), dim3(NW * 64), 0, stream, a);
       return;
     }
   }
@@ -1621,8 +1628,11 @@ hipError_t launch_as(const AttPlan& p, const AttArgs& a, hipStream_t stream) {
 //    tiles of 128 746; 64 rows, 256 to a head, 57 and 64), the others of 128
 //    (1024 rows behind 1024, 4 sequences, 51, tiles of 256 59, which then are fewer
 //    than compute units; larger calls were not compared).
-int tile_rows_of(int dtype, int format, int head_dim, int64_t rows) {
-  if (dtype == EVO_BF16 && rows >= lds_rows(format, head_dim)) return head_dim == 128 && rows > 128 ? 256 : 128;
+//  * fp4 takes the other codes' choices, which were not measured over it, but for a
+//    single block of keys, which does not go through LDS (32 over 8 heads of 128: 4000
+//    rows of 4 sequences over 64 positions 76, LDS 118; 1000 rows of 8 30 and 55).
+int tile_rows_of(int dtype, int format, int head_dim, int64_t rows, bool rest) {
+  if (dtype == EVO_BF16 && rows >= lds_rows(format, head_dim) && !rest) return head_dim == 128 && rows > 128 ? 256 : 128;
   return rows <= 16 || !two_row_blocks(format, head_dim) ? 16 : 32;
 }
 
@@ -1635,7 +1645,9 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   AttPlan p = {};
   const int group = n_heads / n_kv_heads;
   const int64_t rows = (int64_t)r.max_rows * group;  // of one sequence and key/value head
-  p.tile_rows = tile_rows_of(dtype, format, head_dim, rows);
+  const int64_t blocks = ((int64_t)max_length + kKeys - 1) / kKeys;
+  p.rest = dtype == EVO_BF16 && format == EVO_CACHE_FP4 && (rows <= 8 || blocks <= 1);
+  p.tile_rows = tile_rows_of(dtype, format, head_dim, rows, p.rest);
   // row tiles: as many for every sequence, or packed by the rows before
   const int64_t even = (rows + p.tile_rows - 1) / p.tile_rows;
   const int64_t packed = (int64_t)r.n_rows * group / p.tile_rows + r.n_seqs;
@@ -1645,7 +1657,6 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   } else {
     p.n_tiles = (int)packed;
   }
-  const int64_t blocks = ((int64_t)max_length + kKeys - 1) / kKeys;
   const int64_t wgs = (int64_t)p.n_tiles * n_kv_heads;
   // parts of the keys: two workgroups for every compute unit (one of eight
   // waves), each with a few blocks for every wave (part_blocks)
@@ -1654,7 +1665,7 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   // and no more parts than a part has blocks (one token over 65536 positions, 8 heads of
   // 128, 27.0 us with 64 parts, 22.0 with 32; 12 heads of 64 over 16384 16.6 with 42,
   // 11.4 with 16; 6 ragged sequences of up to 65001 65 with two, 54 with three, 59 with
-  // four; 6 equally long ones 113, 90 and 104).
+  // four; 6 equally long ones 113, 90 and 104; all with bf16 queries).
   if (format == EVO_CACHE_FP4 && p.tile_rows <= 32) {
     each = 3;
     most = std::min(most, (int64_t)std::ceil(std::sqrt((double)blocks)));
@@ -1669,7 +1680,6 @@ AttPlan plan_attention(int dtype, int format, int head_dim, int n_heads, int n_k
   // over 27 positions 491 us with four waves and 129 with one, int8 136 and 48;
   // over 250 93 and 52, int8 27 and 20; over 1000 126 and 111, int8 35 and 43)
   if (p.tile_rows <= 32 && p.n_split == 1 && wgs >= 4 * (int64_t)n_cu && blocks <= 8) p.waves = 1;
-  p.rest = dtype == EVO_BF16 && format == EVO_CACHE_FP4 && rows <= 8 && p.waves > 1 && wgs * p.n_split <= n_cu;
   if (p.n_split > 1) {
     p.ml_floats = wgs * p.n_split * p.tile_rows * 2;
     p.part_floats = wgs * p.n_split * p.tile_rows * head_dim;

@@ -1,4 +1,5 @@
-"""The softmax's terms of small bf16 calls over 4-bit caches have twice bf16's bits:
+"""The softmax's terms of bf16 calls over 4-bit caches have twice bf16's bits where a
+sequence has few rows to a key/value head or few positions, whatever else the call holds:
 against the definition in 64 bits, with a bound that terms of bf16's own 8 bits break
 (shown on the CPU)."""
 import numpy as np
@@ -13,10 +14,14 @@ from tests.memory_util import EPS16, EPS32, f64, i32, table_for
 FP4, BF16 = torch.float4_e2m1fn_x2, torch.bfloat16
 SCALE = 0.125
 
-# up to 8 rows to a key/value head, and few enough workgroups not to fill the device
+# up to 8 rows to a key/value head, few workgroups and enough to fill the device; any
+# number of rows over up to 64 positions
 CALLS = [  # rows, lengths, heads, kv_heads, dh
     ([1], [1], 4, 4, 64), ([1], [40], 2, 2, 32), ([2], [250], 8, 2, 64), ([1, 1, 1], [64, 3, 300], 4, 4, 64),
-    ([8], [200], 2, 2, 128), ([1], [600], 4, 4, 64), ([3], [1000], 4, 2, 32), ([1], [900], 8, 1, 128)]
+    ([8], [200], 2, 2, 128), ([1], [600], 4, 4, 64), ([3], [1000], 4, 2, 32), ([1], [900], 8, 1, 128),
+    ([1] * 96, [1 + 37 * s % 250 for s in range(96)], 12, 12, 64), ([1] * 34, [700 - 19 * s for s in range(34)], 32, 8, 128),
+    ([2, 1] * 20, [1300 - 60 * (s % 7) for s in range(40)], 8, 8, 32), ([7] * 70, [5 + s for s in range(70)], 4, 4, 64),
+    ([17], [30], 8, 2, 32), ([40, 300], [64, 7], 2, 2, 64), ([150], [60], 2, 2, 128), ([60, 1], [3, 64], 4, 1, 128)]
 
 
 class Small:
@@ -36,27 +41,33 @@ class Small:
         self.q = torch.randint(-3, 4, (sum(rows), heads, dh), generator=gen).to(BF16)
 
     def parts(self):
-        """(queries, keys, values) of each sequence."""
-        k, v = (M.e2m1_of_bytes(x.numpy(), axis) for x, axis in ((self.k, 3), (self.v, 2)))
+        """(scores [heads][rows][keys], values' codes and scales by query head
+        [heads][keys][dh] and [heads][keys]) of each sequence."""
+        k, v = M.e2m1_of_bytes(self.k.numpy(), 3), M.e2m1_of_bytes(self.v.numpy(), 2)
         at = 0
         for s, (n, length) in enumerate(zip(self.rows, self.lengths)):
-            yield f64(self.q[at:at + n]), *M.gather(k, v, f64(self.ks), f64(self.vs), self.tab, s, length), s
+            j = np.arange(length)
+            page, slot = self.tab[s][j // 64], j % 64
+            group = self.heads // k.shape[1]
+            keys, values = (np.repeat(x.swapaxes(0, 1), group, 0) for x in (k[page, :, slot] * 0.5, v[page, :, :, slot]))
+            scale = np.repeat(f64(self.vs)[page, :, slot].T, group, 0)
+            yield SCALE * (f64(self.q[at:at + n]).swapaxes(0, 1) @ keys.swapaxes(1, 2)), values, scale
             at += n
 
     def reference(self):
         """(outputs, bounds).  A term is off by 2^-16 of itself, or its exponential's
         2^-22, its exponent (EPS32 of the score a few times) and the sums of as many
-        terms as there are keys; the output is rounded once,
-        by half a step of its size."""
+        terms as there are keys; the output is rounded once, by half a step of its size."""
         outs, bounds = [], []
-        for q, k, v, _ in self.parts():
-            out, _ = M.attend(q, k, v, 0, SCALE)
-            size, _ = M.attend(q, k, np.abs(v), 0, SCALE)
-            z = np.max(np.sum(np.abs(q), -1)) * np.max(np.abs(k), initial=0) * SCALE
-            outs.append(out)
-            near = size * (2.0 ** -16 + 2.0 ** -22 + 16 * EPS32 * z + 2 * (len(k) + 64) * EPS32)
+        for z, v, scale in self.parts():
+            p = np.exp(z - z.max(-1, keepdims=True))
+            p /= p.sum(-1, keepdims=True)
+            v = v * scale[..., None]
+            out, size, keys = p @ v, p @ np.abs(v), z.shape[-1]
+            near = size * (2.0 ** -16 + 2.0 ** -22 + 16 * EPS32 * np.max(np.abs(z)) + 2 * (keys + 64) * EPS32)
             half_step = EPS16 * 2.0 ** np.floor(np.log2(np.maximum(np.abs(out) + near, 1e-30)))
-            bounds.append(near + half_step)
+            outs.append(out.swapaxes(0, 1))
+            bounds.append((near + half_step).swapaxes(0, 1))
         return np.concatenate(outs), np.concatenate(bounds)
 
     def rounded(self, bits16):
@@ -65,19 +76,11 @@ class Small:
         def half(x):
             return torch.from_numpy(x).to(BF16).double().numpy()
         outs = []
-        for q, k, v, s in self.parts():
-            place = [M.place(self.tab, 64, s, j) for j in range(len(k))]
-            scale = np.stack([f64(self.vs)[pg, :, sl] for pg, sl in place])      # [keys][kv_heads]
-            group = self.heads // k.shape[1]
-            out = np.zeros(q.shape)
-            for i in range(q.shape[0]):
-                for h in range(self.heads):
-                    z = SCALE * (k[:, h // group] @ q[i, h])
-                    p = np.exp(z - np.max(z))
-                    t = p * scale[:, h // group]
-                    held = half(t) if not bits16 else half(t) + half(t - half(t))
-                    out[i, h] = (held / scale[:, h // group]) @ v[:, h // group] / np.sum(p)
-            outs.append(half(out))
+        for z, v, scale in self.parts():
+            p = np.exp(z - z.max(-1, keepdims=True))
+            t = p * scale[:, None]
+            held = half(t) if not bits16 else half(t) + half(t - half(t))
+            outs.append(half(held @ v / p.sum(-1, keepdims=True)).swapaxes(0, 1))
         return np.concatenate(outs)
 
     def run(self, dev):
@@ -96,7 +99,7 @@ def test_the_bound_tells_16_bits_from_8(i):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("i", range(len(CALLS)))
-def test_terms_of_small_calls(i):
+def test_terms_of_16_bits(i):
     dev = device()
     say(f"[gpu] terms of rows {CALLS[i]}")
     call = Small(*CALLS[i], seed=i)
