@@ -698,8 +698,9 @@ int evo_chunk_attention(const evo_kv_cache* cache, const evo_kv_rows* rows, cons
  * Inference operators like the ones above; asynchronous on hip_stream, device
  * memory of the current device, no workspace.
  *
- * A matrix [rows][columns]: row stride in elements, the columns contiguous.  Rows
- * aligned to 16 bytes take the wide loads. */
+ * A matrix [rows][columns]: row stride in elements, the columns contiguous.  Norms take
+ * wide loads and stores where d is a multiple of 8 and every row and array of the call is
+ * aligned to 16 bytes, products wide stores where out's rows are. */
 typedef struct {
   void* data;
   int64_t row_stride;

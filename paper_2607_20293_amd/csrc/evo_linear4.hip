@@ -127,8 +127,9 @@ __device__ __forceinline__ f32x4 multiply_chunk(u32x4 codes, float scale, const 
 
 // Workgroup (16 C weight rows, 16 rows of x): its eight waves take chunks of 128
 // values in turn, straight from memory to registers, and join their sums through LDS,
-// in order.  What bounds it: memory (one row, 8192 to 8192 features: 13 us of the 7.2
-// that the codes take at a copy's rate and the 2.8 of the smallest launch).  C is 2
+// in order.  What bounds it: memory (one row, 8192 to 8192 features: 13 us with weights
+// that come from memory, 12 where the last cache has them, of the 7.2 that the codes take
+// at a copy's rate and the 2.8 of the smallest launch).  C is 2
 // where that leaves a workgroup for each compute unit, because x is then read half as
 // often (16 rows, 8192 to 8192: 19.6 us, so 27), else 1 (one row, 4096 to 4096: 5.6,
 // so 7.2).  Requesting two or four chunks at once changes nothing: three to four

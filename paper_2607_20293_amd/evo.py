@@ -1080,7 +1080,7 @@ class Weights4:
         """(codes, scales) of weights w [n_out][n_in], on w's device: the scale of a
         group is the least power of two that brings its largest magnitude to 6 or
         below (2^-126 to 2^125), the codes are the nearest, ties to even.  Weights
-        must be finite floats of 32 bits."""
+        must be finite in 32 bits, to which those of 64 are rounded first."""
         if w.dim() != 2 or not w.dtype.is_floating_point:
             raise ValueError("w must be [n_out][n_in] of floats")
         n_out, n_in = w.shape
@@ -1108,7 +1108,8 @@ class Weights4:
         return cls(*cls.coded(w), w.shape[1])
 
     def values(self):
-        """The weights that the codes stand for, float32 [n_out][n_in]."""
+        """The weights that the codes stand for, float32 [n_out][n_in] (infinities
+        from 2^128 on)."""
         b = self.codes.view(torch.uint8)
         grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=b.device)
         grid = torch.cat([grid, -grid])
